@@ -395,6 +395,104 @@ dfss_status dfss_attention_backward(const void *dO, const void *Q, const void *K
  * dfss_attention_staged runs the stage kernels), and dense_attention_fused is available as
  * the matching full-attention kernel. */
 
+/* ---- around a decoder's attention: head norms, rotary positions, a cache ---------------- */
+/* What makes the queries and keys of the calls above, and a paged cache of 8 bits for generation with the
+ * attention that reads it.  All sizes and strides are checked on the host; what lies in device memory
+ * (positions, page numbers, lengths, row offsets) is not: values out of range are cut as each call says,
+ * and no value of theirs makes a call read or write outside the arrays.  Inputs are finite. */
+
+/* Rows of H heads, d elements each, as a projection leaves them: the row of head h, token t of batch
+ * element b starts `b * batch + t * token + h * head` elements behind data.  data and the three strides
+ * (>= 0) in bytes are multiples of 16. */
+typedef struct {
+    void *data;       /* device                                                                   */
+    int32_t H;
+    int64_t batch, token, head;
+} dfss_rows;
+
+/* Rotation of the first `rot` elements of a row by its token's angles (rotary positions):
+ *   y1 = x1 cos - x2 sin,   y2 = x2 cos + x1 sin
+ * for the pairs (x[i], x[i + rot/2]), or (x[2i], x[2i+1]) with interleaved != 0; angle i of position p is
+ * given by cos[p][i], sin[p][i].  The other elements stay.  rot: a multiple of 16, 16 <= rot <= d. */
+typedef struct {
+    const float *cos, *sin;  /* device, float32 [n_pos, rot/2] row-major, 16-byte aligned               */
+    const int32_t *pos;      /* device, position of every token, 4-byte aligned; NULL: its place in its  */
+                             /* sequence.  Positions outside [0, n_pos) take the nearest one inside.     */
+    int32_t n_pos, rot, interleaved;
+} dfss_rotary;
+
+/* Norm of every head's query and key and their rotation, in one pass:
+ *   z = x (mean(x^2) + eps)^(-1/2) w,   y = rotated z
+ * for every row x of Q (weight wq) and of K (weight wk).  wq, wk: device, [d], the shape's dtype, 16-byte
+ * aligned; NULL: no norm, z = x.  rotary: NULL for none; its pos is [B, Lq].  K and Ko may both be NULL.
+ * Uses B, H (= Q->H), Lq (tokens of a batch element, for queries and keys alike), d (64, 128) and dtype
+ * (DFSS_BF16, DFSS_F32) of the shape.  eps: finite and >= 0 (a row of zeros needs eps > 0).
+ * Qo, Ko: where the results go; with batch = H*Lq*d, token = d, head = Lq*d that is the [B*H, Lq, d] of the
+ * attention calls.  Results may take the place of the inputs (same data and strides); other overlaps are
+ * not allowed.  32-bit arithmetic, one rounding at the end. */
+dfss_status dfss_qk_norm_rotate(const dfss_rows *Q, const dfss_rows *K, const void *wq, const void *wk,
+                                const dfss_rotary *rotary, const dfss_shape *s, float eps, const dfss_rows *Qo,
+                                const dfss_rows *Ko, void *stream);
+/* Its gradients.  dQo, dKo: gradients of the results; Q, K, the weights and rotary as in the forward call (Q and K
+ * are read where there is a weight).  dQ, dK: out, gradients of Q and K; they may take the place of dQo and dKo or
+ * of Q and K as above.  dwq, dwk: out, float32 [d], 4-byte aligned, gradients of the weights (ignored where the weight
+ * is NULL).  ws: device, 256-byte aligned, dfss_qk_norm_workspace_bytes(s) bytes, contents undefined before and after; without
+ * weights it may be NULL.  Sums over rows in 32 bits, in a fixed order. */
+size_t dfss_qk_norm_workspace_bytes(const dfss_shape *s);
+dfss_status dfss_qk_norm_rotate_backward(const dfss_rows *dQo, const dfss_rows *dKo, const dfss_rows *Q,
+                                         const dfss_rows *K, const void *wq, const void *wk, const dfss_rotary *rotary,
+                                         const dfss_shape *s, float eps, const dfss_rows *dQ, const dfss_rows *dK,
+                                         void *dwq, void *dwk, void *ws, size_t ws_bytes, void *stream);
+
+/* A cache of keys and values in pages of `page` tokens (16, 32, 64 or 128), 8 bits a value: e4m3 codes
+ * [n_pages, Hk, page, d] and for every page and head one scale, a power of two; a code stands for its e4m3 value times
+ * the scale.  Token i of sequence b lies in row i % page of page table[b][i / page].  len[b]: tokens of the
+ * sequence.  Page numbers outside [0, n_pages) are no pages: tokens of theirs are not kept, and no query
+ * sees them.  Entries of the table behind a sequence's last token are not read. */
+typedef struct {
+    void *k, *v;              /* device, uint8, 16-byte aligned                                          */
+    void *k_scale, *v_scale;  /* device, float32 [n_pages, Hk], 4-byte aligned                           */
+    const int32_t *table;     /* device, [B, width], 4-byte aligned                                      */
+    const int32_t *len;       /* device, [B], 4-byte aligned                                             */
+    int32_t n_pages, Hk, page, width;
+} dfss_cache;
+
+/* Appends new tokens: rows of K and V, of `rows` tokens in all (strides token and head; batch is not used).
+ * cu: device, int32 [B + 1], 4-byte aligned: the tokens of sequence b are rows cu[b] .. cu[b+1] - 1, none allowed; cu[0] = 0,
+ * not decreasing, at most `rows` (values outside [0, rows] are cut).  cu == NULL: Lq tokens each (rows = B * Lq).
+ * len holds the lengths WITH the new tokens, so that the n tokens of sequence b become its tokens
+ * len[b] - n .. len[b] - 1; those whose place would be negative, or Lk or more (a length of at most width * page),
+ * are not kept.  Keys are normed with w ([d], bfloat16, 16-byte aligned; NULL: not) and rotated (rotary: NULL for none; its pos is
+ * [rows], NULL: the token's place) on the way, in 32 bits, and rounded once.
+ * The scale of a page and head becomes 2^ceil(log2(amax / 448)), at least 2^-64, over the appended values; where
+ * the page holds earlier tokens of the sequence it is at least what it was, and if it grows their codes are
+ * rounded again (nearest-even) to the new scale.  Nothing else of the cache is written.  A page that several sequences
+ * share (a common prefix) is read by any number of them; appending to it from more than one of them in
+ * one call, or while another call reads it, is not ordered.
+ * Uses B, H (= Hk = K->H = V->H), Lq (>= 1; read where cu is NULL), Lk (<= 2^24) and d of the shape; DFSS_BF16 rows. */
+dfss_status dfss_cache_append(const dfss_rows *K, const dfss_rows *V, int32_t rows, const int32_t *cu,
+                              const dfss_cache *cache, const void *w, const dfss_rotary *rotary, const dfss_shape *s,
+                              float eps, void *stream);
+
+/* Attention of the last tokens' queries over the cache: O = softmax(scale q K^T, N of every M consecutive keys kept)
+ * V, or over all keys (dense_attention_cached; N, M ignored).  Q: rows as K in the call above, H a
+ * multiple of Hk: heads h*G .. h*G + G - 1 read key head h, G = H / Hk.  cu as above.  Lq: the most queries of a
+ * sequence, Lk: the most keys; queries from Lq on are not computed, keys from Lk on not seen.  With causal != 0 the n queries of
+ * sequence b are its last n tokens: query i sees keys 0 .. len[b] - n + i; otherwise all len[b].  A query that
+ * sees no key gets 0.  Selection as everywhere: larger score wins, equal scores -> lower key; hidden keys lose to all others and weigh 0.
+ * O: device, bfloat16 [rows, H, d], 16-byte aligned; rows of no sequence are not written.
+ * ws: device, 256-byte aligned, dfss_cached_workspace_bytes(s, cache) bytes (may be 0, then it may be NULL), contents
+ * undefined before and after.  How many workgroups share the keys of a sequence depends on the shape and Hk
+ * alone: with a large Lk (room to grow under a captured graph) short sequences are shared out by their own length.
+ * Uses B, H, Lq, Lk (<= 2^24, at most width * page), d, N, M of the shape; DFSS_BF16.  One kernel, or two where keys are shared. */
+size_t dfss_cached_workspace_bytes(const dfss_shape *s, const dfss_cache *cache);
+dfss_status dfss_attention_cached(const dfss_rows *Q, int32_t rows, const int32_t *cu, const dfss_cache *cache,
+                                  const dfss_shape *s, float scale, int32_t causal, void *O, void *ws, size_t ws_bytes,
+                                  void *stream);
+dfss_status dense_attention_cached(const dfss_rows *Q, int32_t rows, const int32_t *cu, const dfss_cache *cache,
+                                   const dfss_shape *s, float scale, int32_t causal, void *O, void *ws, size_t ws_bytes,
+                                   void *stream);
+
 /* ---- metadata order ---------------------------------------------------------------- */
 /* Canonical order: uint16 [B*H, Lq, Lk/16], word w of a row = codes of key runs
  * 4w..4w+3, code = p_lo | p_hi << 2 with p the kept key index mod 4 (the 2-bit

@@ -35,6 +35,8 @@ EXPORTS = (
     "dfss_attention_mask", "dense_attention_fused_mask",
     "dfss_attention_varlen",
     "dfss_ragged_split_workspace_bytes", "dfss_attention_ragged_split",
+    "dfss_qk_norm_rotate", "dfss_qk_norm_workspace_bytes", "dfss_qk_norm_rotate_backward",
+    "dfss_cache_append", "dfss_cached_workspace_bytes", "dfss_attention_cached", "dense_attention_cached",
 )
 # exported for the library's own tests only (csrc/dfss_internal.h)
 INTERNAL_EXPORTS = ("dfss_internal_attention_variant",)
@@ -52,6 +54,19 @@ class DfssError(RuntimeError):
 
 class _CShape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("B", "H", "Lq", "Lk", "d", "N", "M", "dtype")]
+
+
+class _CRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("H", ctypes.c_int32)] + [(n, ctypes.c_int64) for n in ("batch", "token", "head")]
+
+
+class _CRotary(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("cos", "sin", "pos")] + [(n, ctypes.c_int32) for n in ("n_pos", "rot", "interleaved")]
+
+
+class _CCache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "table", "len")] + \
+               [(n, ctypes.c_int32) for n in ("n_pages", "Hk", "page", "width")]
 
 
 class _Call:
@@ -184,6 +199,20 @@ def load_library():
         L.dfss_attention_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, sp, f32, vp, vp, vp, vp, sz, vp]
         L.dfss_meta_to_canonical.argtypes = [vp, sp, vp, vp]
         L.dfss_meta_from_canonical.argtypes = [vp, sp, vp, vp]
+        rows, rot, cache = (ctypes.POINTER(c) for c in (_CRows, _CRotary, _CCache))
+        n32 = ctypes.c_int32
+        L.dfss_qk_norm_rotate.argtypes = [rows, rows, vp, vp, rot, sp, f32, rows, rows, vp]
+        L.dfss_qk_norm_workspace_bytes.argtypes = [sp]
+        L.dfss_qk_norm_workspace_bytes.restype = sz
+        L.dfss_qk_norm_rotate_backward.argtypes = [rows, rows, rows, rows, vp, vp, rot, sp, f32, rows, rows, vp, vp, vp, sz, vp]
+        L.dfss_cache_append.argtypes = [rows, rows, n32, vp, cache, vp, rot, sp, f32, vp]
+        L.dfss_cached_workspace_bytes.argtypes = [sp, cache]
+        L.dfss_cached_workspace_bytes.restype = sz
+        L.dfss_attention_cached.argtypes = [rows, n32, vp, cache, sp, f32, n32, vp, vp, sz, vp]
+        L.dense_attention_cached.argtypes = [rows, n32, vp, cache, sp, f32, n32, vp, vp, sz, vp]
+        for name in ("dfss_qk_norm_rotate", "dfss_qk_norm_rotate_backward", "dfss_cache_append", "dfss_attention_cached",
+                     "dense_attention_cached"):
+            getattr(L, name).restype = ctypes.c_int
         for name in ("dfss_sddmm_prune", "dfss_sparse_softmax", "dfss_spmm", "dfss_attention",
                      "dense_attention", "dense_attention_fused", "dfss_meta_to_canonical", "dfss_meta_from_canonical",
                      "dfss_sddmm_prune_bias", "dfss_attention_bias", "dense_attention_bias",
@@ -749,3 +778,193 @@ def dfss_meta_from_canonical(canon, s: Shape, meta=None):
     st = load_library().dfss_meta_from_canonical(_meta(canon, s), s._call.ref, _meta(meta, s), _stream())
     _check("dfss_meta_from_canonical", st)
     return meta
+
+
+# ---- around a decoder's attention ------------------------------------------------------------------------------
+
+
+def _device(t: torch.Tensor, dtype, what: str) -> int:
+    """Pointer of a tensor of the given type (or one of several) on the current device."""
+    if t.dtype is not dtype and not (isinstance(dtype, tuple) and t.dtype in dtype):
+        raise ValueError(f"{what}: expected {dtype}, got {t.dtype}")
+    if not t.is_cuda or t.device.index != torch._C._cuda_getDevice():
+        raise ValueError(f"{what}: expected a tensor on the current device, got one on {t.device}")
+    return t.data_ptr()
+
+
+def _array(t: torch.Tensor, dtype, shape, what: str) -> int:
+    """The same of a contiguous one of the given shape."""
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous tensor {list(shape)}, got {list(t.shape)}")
+    return _device(t, dtype, what)
+
+
+class Rotary:
+    """Rotary positions (``dfss_rotary``): cos, sin float32 [n_pos, rot/2]; pos int32, the position of every token of a
+    call (None: its place in its sequence); pairs (i, i + rot/2), or neighbours if ``interleaved``.  Keeps its tensors."""
+    __slots__ = ("cos", "sin", "pos", "interleaved", "_c", "_ref")
+
+    def __init__(self, cos, sin, pos=None, interleaved: bool = False):
+        if cos.dim() != 2:
+            raise ValueError(f"cos, sin: expected [n_pos, rot/2], got {list(cos.shape)}")
+        self.cos, self.sin, self.pos, self.interleaved = cos, sin, pos, interleaved
+        self._c = _CRotary(_array(cos, torch.float32, cos.shape, "cos"), _array(sin, torch.float32, cos.shape, "sin"),
+                           None if pos is None else _array(pos, torch.int32, pos.shape, "pos"),
+                           cos.shape[0], 2 * cos.shape[1], int(bool(interleaved)))
+        self._ref = ctypes.byref(self._c)
+
+
+def _rotary(r: Rotary | None, tokens: int):
+    if r is None:
+        return None
+    if r.pos is not None and r.pos.numel() != tokens:
+        raise ValueError(f"pos: expected {tokens} positions, got {r.pos.numel()}")
+    return r._ref
+
+
+class Cache:
+    """A paged cache of 8 bits (``dfss_cache``): k, v uint8 or float8_e4m3fn [n_pages, Hk, page, d], their scales float32
+    [n_pages, Hk], table int32 [B, width], len int32 [B].  Keeps its tensors."""
+    __slots__ = ("k", "v", "k_scale", "v_scale", "table", "len", "_c", "_ref")
+
+    def __init__(self, k, v, k_scale, v_scale, table, len):
+        if k.dim() != 4 or table.dim() != 2:
+            raise ValueError(f"expected k, v [n_pages, Hk, page, d] and table [B, width], got {list(k.shape)}, {list(table.shape)}")
+        self.k, self.v, self.k_scale, self.v_scale, self.table, self.len = k, v, k_scale, v_scale, table, len
+        codes = (torch.uint8, torch.float8_e4m3fn)
+        self._c = _CCache(_array(k, codes, k.shape, "k"), _array(v, codes, k.shape, "v"),
+                          _array(k_scale, torch.float32, k.shape[:2], "k_scale"), _array(v_scale, torch.float32, k.shape[:2], "v_scale"),
+                          _array(table, torch.int32, table.shape, "table"), _array(len, torch.int32, table.shape[:1], "len"),
+                          k.shape[0], k.shape[1], k.shape[2], table.shape[1])
+        self._ref = ctypes.byref(self._c)
+
+
+def _rows(t: torch.Tensor | None, shape, dtype, what: str, out: bool = False):
+    """Rows of heads.  [batch, token, head, d] with any strides of the first three, or, for shape[0] * heads rows of a batch
+    element each, the contiguous [batch * head, token, d] of the attention calls; [token, head, d] where shape has no batch.
+    shape: (batch, token, d) or (token, d)."""
+    if t is None:
+        return None
+    p, n, x = _device(t, dtype, what), t.shape, t.stride()
+    d = shape[-1]
+    if len(shape) == 2:
+        if t.dim() != 3 or n[0] != shape[0] or n[2] != d or x[2] != 1:
+            raise ValueError(f"{what}: expected [{shape[0]}, heads, {d}] with elements side by side, got {list(n)}")
+        H, batch, token, head = n[1], 0, x[0] if n[0] > 1 else 0, x[1] if n[1] > 1 else 0
+    elif t.dim() == 3:
+        if n[0] % shape[0] or n[1] != shape[1] or n[2] != d or not t.is_contiguous():
+            raise ValueError(f"{what}: expected a contiguous [{shape[0]} * heads, {shape[1]}, {d}], got {list(n)}")
+        H = n[0] // shape[0]
+        batch, token, head = H * shape[1] * d, d, shape[1] * d
+    else:
+        if t.dim() != 4 or n[0] != shape[0] or n[1] != shape[1] or n[3] != d or x[3] != 1:
+            raise ValueError(f"{what}: expected [{shape[0]}, {shape[1]}, heads, {d}] with elements side by side, got {list(n)}")
+        H, batch, token, head = n[2], x[0] if n[0] > 1 else 0, x[1] if n[1] > 1 else 0, x[2] if n[2] > 1 else 0
+    if out and any(k > 1 and y == 0 for k, y in zip(n, x)):
+        raise ValueError(f"{what}: a result cannot share rows")
+    return _CRows(p, H, batch, token, head)
+
+
+def _weight(w: torch.Tensor | None, dtype, d: int, what: str):
+    return None if w is None else _array(w, dtype, (d,), what)
+
+
+def dfss_qk_norm_rotate(Q, K, wq, wk, rotary: Rotary | None, s: Shape, eps: float = 1e-6, Qo=None, Ko=None):
+    """Norm of every head's query and key (weights wq, wk [d], None: none) and rotation to the token's position.
+    Q, K: [B, Lq, heads, d] with any strides (or [B * heads, Lq, d]); K may be None.  Returns Qo, Ko, [B * heads, Lq, d] as
+    the attention calls take them unless given."""
+    t, shape = s._call.torch_dtype, (s.B, s.Lq, s.d)
+    q, k = _rows(Q, shape, t, "Q"), _rows(K, shape, t, "K")
+    if Qo is None:
+        Qo = torch.empty((s.B * q.H, s.Lq, s.d), dtype=t, device=Q.device)
+    if Ko is None and K is not None:
+        Ko = torch.empty((s.B * k.H, s.Lq, s.d), dtype=t, device=Q.device)
+    st = load_library().dfss_qk_norm_rotate(q, k, _weight(wq, t, s.d, "wq"), _weight(wk, t, s.d, "wk"),
+                                            _rotary(rotary, s.B * s.Lq), s._call.ref, eps, _rows(Qo, shape, t, "Qo", True),
+                                            _rows(Ko, shape, t, "Ko", True), _stream())
+    _check("dfss_qk_norm_rotate", st)
+    return Qo, Ko
+
+
+def dfss_qk_norm_workspace_bytes(s: Shape) -> int:
+    return int(load_library().dfss_qk_norm_workspace_bytes(s._call.ref))
+
+
+def dfss_qk_norm_rotate_backward(dQo, dKo, Q, K, wq, wk, rotary: Rotary | None, s: Shape, eps: float = 1e-6, dQ=None, dK=None,
+                                 dwq=None, dwk=None, ws=None):
+    """Gradients of dfss_qk_norm_rotate: (dQ, dK, dwq, dwk), those of Q and K [B, Lq, heads, d] unless given, those of the
+    weights float32 [d] (None where there is no weight)."""
+    t, shape = s._call.torch_dtype, (s.B, s.Lq, s.d)
+    q, k = _rows(Q, shape, t, "Q"), _rows(K, shape, t, "K")
+    if dQ is None:
+        dQ = torch.empty((s.B, s.Lq, q.H, s.d), dtype=t, device=Q.device)
+    if dK is None and K is not None:
+        dK = torch.empty((s.B, s.Lq, k.H, s.d), dtype=t, device=Q.device)
+    if dwq is None and wq is not None:
+        dwq = torch.empty(s.d, dtype=torch.float32, device=Q.device)
+    if dwk is None and wk is not None and K is not None:
+        dwk = torch.empty(s.d, dtype=torch.float32, device=Q.device)
+    if ws is None and (dwq is not None or dwk is not None):
+        ws = _alloc_bytes(dfss_qk_norm_workspace_bytes(s), Q.device)
+    st = load_library().dfss_qk_norm_rotate_backward(
+        _rows(dQo, shape, t, "dQo"), _rows(dKo, shape, t, "dKo"), q, k, _weight(wq, t, s.d, "wq"), _weight(wk, t, s.d, "wk"),
+        _rotary(rotary, s.B * s.Lq), s._call.ref, eps, _rows(dQ, shape, t, "dQ", True), _rows(dK, shape, t, "dK", True),
+        _weight(dwq, torch.float32, s.d, "dwq"), _weight(dwk, torch.float32, s.d, "dwk"), _ptr(ws),
+        0 if ws is None else ws.numel() * ws.element_size(), _stream())
+    _check("dfss_qk_norm_rotate_backward", st)
+    return dQ, dK, dwq, dwk
+
+
+def _offsets(cu: torch.Tensor | None, s: Shape):
+    return None if cu is None else _array(cu, torch.int32, (s.B + 1,), "cu")
+
+
+def _cache(c: Cache, s: Shape):
+    if c.table.shape[0] != s.B or c.k.shape[3] != s.d:
+        raise ValueError(f"cache: expected {s.B} sequences and head size {s.d}, got {c.table.shape[0]} and {c.k.shape[3]}")
+    if c.k.device.index != torch._C._cuda_getDevice():
+        raise ValueError(f"cache: expected one on the current device, got one on {c.k.device}")
+    return c._ref
+
+
+def dfss_cache_append(K, V, cu, cache: Cache, w, rotary: Rotary | None, s: Shape, eps: float = 1e-6):
+    """New tokens into the cache: K, V [tokens, Hk, d] with any strides of the first two, tokens cu[b] .. cu[b+1] - 1 for
+    sequence b (cu None: Lq each); cache.len holds the lengths with them.  Keys are normed (w None: not) and rotated on
+    the way.  s: B sequences, H = Hk key heads, at most Lk tokens a sequence."""
+    n = K.shape[0]
+    st = load_library().dfss_cache_append(_rows(K, (n, s.d), torch.bfloat16, "K"), _rows(V, (n, s.d), torch.bfloat16, "V"), n,
+                                          _offsets(cu, s), _cache(cache, s), _weight(w, torch.bfloat16, s.d, "w"),
+                                          _rotary(rotary, n), s._call.ref, eps, _stream())
+    _check("dfss_cache_append", st)
+
+
+def dfss_cached_workspace_bytes(s: Shape, cache: Cache) -> int:
+    return int(load_library().dfss_cached_workspace_bytes(s._call.ref, cache._ref))
+
+
+def _attention_cached(name: str, Q, cu, cache: Cache, s: Shape, scale: float, causal: bool, O, ws):
+    n = Q.shape[0]
+    q, c = _rows(Q, (n, s.d), torch.bfloat16, "Q"), _cache(cache, s)
+    if O is None:
+        O = torch.empty((n, q.H, s.d), dtype=torch.bfloat16, device=Q.device)
+    L = load_library()
+    if ws is None:
+        need = L.dfss_cached_workspace_bytes(s._call.ref, c)
+        ws = _alloc_bytes(need, Q.device) if need else None
+    st = getattr(L, name)(q, n, _offsets(cu, s), c, s._call.ref, scale, int(bool(causal)),
+                          _array(O, torch.bfloat16, (n, q.H, s.d), "O"), _ptr(ws),
+                          0 if ws is None else ws.numel() * ws.element_size(), _stream())
+    _check(name, st)
+    return O
+
+
+def dfss_attention_cached(Q, cu, cache: Cache, s: Shape, scale: float, causal: bool = True, O=None, ws=None):
+    """N:M pruned attention of queries [tokens, H, d] (any strides of the first two; offsets cu as in dfss_cache_append) over
+    the cache; causal: they are the last tokens of their sequences.  s: B sequences, H query heads, at most Lq queries and
+    Lk keys a sequence, N of M.  Returns O [tokens, H, d]."""
+    return _attention_cached("dfss_attention_cached", Q, cu, cache, s, scale, causal, O, ws)
+
+
+def dense_attention_cached(Q, cu, cache: Cache, s: Shape, scale: float, causal: bool = True, O=None, ws=None):
+    """Full attention over the cache; arguments as dfss_attention_cached (N, M ignored)."""
+    return _attention_cached("dense_attention_cached", Q, cu, cache, s, scale, causal, O, ws)

@@ -4,6 +4,8 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <initializer_list>
+
 #include "../../include/dfss.h"
 #include "dfss_internal.h"
 #include "dfss_kernels.hpp"
@@ -661,6 +663,205 @@ dfss_status dfss_meta_from_canonical(const uint16_t *canon, const dfss_shape *s,
     if (misaligned(meta) || misaligned(canon)) return DFSS_ERR_SHAPE;
     return hip_status(dfss::launch_meta_reorder(canon, meta, D.BH, D.Lq, D.Lk / (D.f32 ? 16 : 32), false, !D.f32,
                                                 (hipStream_t)stream));
+}
+
+// ---- around a decoder's attention ---------------------------------------------------------------
+}  // extern "C"
+
+namespace {
+
+inline bool misaligned_to(const void *p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) != 0; }
+
+// Rows of heads; elem: bytes of an element.  (Offsets are formed in 64 bits: strides up to 2^40 elements.)
+dfss_status rows_of(const dfss_rows *r, int elem, dfss::HeadRows *out) {
+    if (!r->data) return DFSS_ERR_NULL;
+    if (r->H <= 0 || r->H > 65535) return DFSS_ERR_SHAPE;
+    const int64_t each = 16 / elem;
+    for (const int64_t x : {r->batch, r->token, r->head})
+        if (x < 0 || x % each != 0 || x > ((int64_t)1 << 40)) return DFSS_ERR_SHAPE;
+    if (misaligned(r->data)) return DFSS_ERR_SHAPE;
+    *out = dfss::HeadRows{r->data, (long)r->batch, (long)r->token, (long)r->head, r->H};
+    return DFSS_OK;
+}
+
+dfss_status rotary_of(const dfss_rotary *r, int d, dfss::RotaryTable *out) {
+    *out = dfss::RotaryTable{nullptr, nullptr, nullptr, 0, 0, 0};
+    if (!r) return DFSS_OK;
+    if (!r->cos || !r->sin) return DFSS_ERR_NULL;
+    if (r->n_pos <= 0 || r->rot < 16 || r->rot > d || r->rot % 16 != 0) return DFSS_ERR_SHAPE;
+    if (misaligned(r->cos) || misaligned(r->sin) || misaligned_to(r->pos, 4)) return DFSS_ERR_SHAPE;
+    *out = dfss::RotaryTable{r->cos, r->sin, r->pos, r->n_pos, r->rot, r->interleaved != 0};
+    return DFSS_OK;
+}
+
+// eps: finite and >= 0 (on the bit pattern, as bad_scale)
+inline bool bad_eps(float x) {
+    uint32_t u;
+    memcpy(&u, &x, sizeof(u));
+    return (u >> 31) != 0 || (u & 0x7F800000u) == 0x7F800000u;
+}
+
+struct HeadNorm {
+    dfss::HeadRows in[2], out[2], grad[2];
+    dfss::RotaryTable rotary;
+    bool f32;
+};
+
+// What both calls check.  The results of K are left empty (H = 0) where there is no K.
+dfss_status head_norm(const dfss_rows *const in[2], const dfss_rows *const out[2], const void *wq, const void *wk,
+                      const dfss_rotary *rotary, const dfss_shape *s, float eps, HeadNorm *N) {
+    if (!in[0] || !out[0] || !s || !in[1] != !out[1]) return DFSS_ERR_NULL;
+    if (s->B <= 0 || s->H <= 0 || s->Lq <= 0 || s->d <= 0) return DFSS_ERR_SHAPE;
+    if (s->dtype != DFSS_BF16 && s->dtype != DFSS_F32) return DFSS_ERR_UNSUPPORTED;
+    if (s->d != 64 && s->d != 128) return DFSS_ERR_UNSUPPORTED;
+    if (bad_eps(eps)) return DFSS_ERR_UNSUPPORTED;
+    N->f32 = s->dtype == DFSS_F32;
+    for (int i = 0; i < 2; ++i) {
+        N->in[i] = N->out[i] = N->grad[i] = dfss::HeadRows{nullptr, 0, 0, 0, 0};
+        if (!in[i]) continue;
+        if (dfss_status st = rows_of(in[i], N->f32 ? 4 : 2, &N->in[i])) return st;
+        if (dfss_status st = rows_of(out[i], N->f32 ? 4 : 2, &N->out[i])) return st;
+        if (N->in[i].H != N->out[i].H) return DFSS_ERR_SHAPE;
+    }
+    if (N->in[0].H != s->H) return DFSS_ERR_SHAPE;
+    if (misaligned(wq) || misaligned(wk)) return DFSS_ERR_SHAPE;
+    // (a launch has fewer than 2^32 threads; a wave takes four rows or more)
+    if ((long long)s->B * s->Lq >= (1LL << 28) / (N->in[0].H + N->in[1].H + 4)) return DFSS_ERR_SHAPE;
+    return rotary_of(rotary, s->d, &N->rotary);
+}
+
+// The cache and what its calls share of the shape.
+dfss_status cache_of(const dfss_cache *c, const dfss_shape *s, dfss::PagedCache *out) {
+    if (!c || !s) return DFSS_ERR_NULL;
+    if (!c->k || !c->v || !c->k_scale || !c->v_scale || !c->table || !c->len) return DFSS_ERR_NULL;
+    if (s->B <= 0 || s->H <= 0 || s->Lq <= 0 || s->Lk <= 0 || s->d <= 0) return DFSS_ERR_SHAPE;
+    if (c->n_pages <= 0 || c->Hk <= 0 || c->Hk > 65535 || c->width <= 0) return DFSS_ERR_SHAPE;
+    if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return DFSS_ERR_SHAPE;
+    if (s->B > (1 << 20) || s->Lq > (1 << 24) || s->Lk > (1 << 24) || (int64_t)c->width * c->page < s->Lk) return DFSS_ERR_SHAPE;
+    if (s->dtype != DFSS_BF16) return DFSS_ERR_UNSUPPORTED;
+    if (s->d != 64 && s->d != 128) return DFSS_ERR_UNSUPPORTED;
+    if (misaligned(c->k) || misaligned(c->v) || misaligned_to(c->k_scale, 4) || misaligned_to(c->v_scale, 4) ||
+        misaligned_to(c->table, 4) || misaligned_to(c->len, 4))
+        return DFSS_ERR_SHAPE;
+    int shift = 4;
+    while ((1 << shift) < c->page) ++shift;
+    *out = dfss::PagedCache{static_cast<uint8_t *>(c->k), static_cast<uint8_t *>(c->v), static_cast<float *>(c->k_scale),
+                            static_cast<float *>(c->v_scale), c->table, c->len, c->n_pages, c->Hk, shift, c->width};
+    return DFSS_OK;
+}
+
+// Heads in whole groups, and at most 2^22 tiles of 16 rows (a launch has fewer than 2^32 threads).
+dfss_status cached_sizes(const dfss_shape *s, int Hk) {
+    if (s->H % Hk != 0) return DFSS_ERR_SHAPE;
+    const long long tiles = ((long long)s->Lq * (s->H / Hk) + 15) / 16;
+    return tiles <= (1LL << 22) / ((long long)s->B * Hk) ? DFSS_OK : DFSS_ERR_SHAPE;
+}
+
+dfss_status attention_cached(const dfss_rows *Q, int32_t rows, const int32_t *cu, const dfss_cache *cache, const dfss_shape *s,
+                             bool dense, float scale, int32_t causal, void *O, void *ws, size_t ws_bytes, void *stream) {
+    dfss::PagedCache C;
+    dfss::HeadRows R;
+    if (!Q || !O) return DFSS_ERR_NULL;
+    if (dfss_status st = cache_of(cache, s, &C)) return st;
+    int mode = 2;
+    if (!dense) {
+        if (s->N == 2 && s->M == 4) mode = 0;
+        else if (s->N == 1 && s->M == 2) mode = 1;
+        else return DFSS_ERR_UNSUPPORTED;
+    }
+    if (bad_scale(scale)) return DFSS_ERR_UNSUPPORTED;
+    if (dfss_status st = rows_of(Q, 2, &R)) return st;
+    if (rows <= 0 || rows > (1 << 27) || R.H != s->H || misaligned(O) || misaligned_to(cu, 4)) return DFSS_ERR_SHAPE;
+    if (!cu && (long long)s->B * s->Lq != rows) return DFSS_ERR_SHAPE;
+    if (dfss_status st = cached_sizes(s, C.Hk)) return st;
+    const size_t need = dfss::cached_workspace_bytes(s->B, s->H, C.Hk, s->Lq, s->Lk, s->d);
+    if (need) {
+        if (!ws) return DFSS_ERR_NULL;
+        if ((reinterpret_cast<uintptr_t>(ws) & (kAlign - 1)) != 0) return DFSS_ERR_SHAPE;
+        if (ws_bytes < need) return DFSS_ERR_WORKSPACE;
+    }
+    return hip_status(dfss::launch_attention_cached(R, rows, cu, s->B, s->Lq, s->Lk, s->d, mode, scale, causal != 0, C, O, ws,
+                                                    (hipStream_t)stream));
+}
+
+}  // namespace
+
+extern "C" {
+
+dfss_status dfss_qk_norm_rotate(const dfss_rows *Q, const dfss_rows *K, const void *wq, const void *wk,
+                                const dfss_rotary *rotary, const dfss_shape *s, float eps, const dfss_rows *Qo,
+                                const dfss_rows *Ko, void *stream) {
+    const dfss_rows *const in[2] = {Q, K}, *const out[2] = {Qo, Ko};
+    HeadNorm N;
+    if (dfss_status st = head_norm(in, out, wq, wk, rotary, s, eps, &N)) return st;
+    return hip_status(dfss::launch_norm_rotate(N.in[0], N.in[1], wq, wk, eps, N.rotary, s->B, s->Lq, s->d, N.f32, N.out[0],
+                                               N.out[1], (hipStream_t)stream));
+}
+
+size_t dfss_qk_norm_workspace_bytes(const dfss_shape *s) {
+    if (!s || (s->d != 64 && s->d != 128)) return 0;
+    return align_up(dfss::norm_rotate_workspace_bytes(s->d));
+}
+
+dfss_status dfss_qk_norm_rotate_backward(const dfss_rows *dQo, const dfss_rows *dKo, const dfss_rows *Q,
+                                         const dfss_rows *K, const void *wq, const void *wk, const dfss_rotary *rotary,
+                                         const dfss_shape *s, float eps, const dfss_rows *dQ, const dfss_rows *dK,
+                                         void *dwq, void *dwk, void *ws, size_t ws_bytes, void *stream) {
+    const dfss_rows *const in[2] = {Q, K}, *const grad[2] = {dQo, dKo}, *const out[2] = {dQ, dK};
+    HeadNorm N;
+    if (dfss_status st = head_norm(in, out, wq, wk, rotary, s, eps, &N)) return st;
+    for (int i = 0; i < 2; ++i) {
+        if (!in[i] != !grad[i]) return DFSS_ERR_NULL;
+        if (!in[i]) continue;
+        if (dfss_status st = rows_of(grad[i], N.f32 ? 4 : 2, &N.grad[i])) return st;
+        if (N.grad[i].H != N.in[i].H) return DFSS_ERR_SHAPE;
+    }
+    if (!K) wk = nullptr;
+    if ((wq && !dwq) || (wk && !dwk)) return DFSS_ERR_NULL;
+    if (misaligned_to(wq ? dwq : nullptr, 4) || misaligned_to(wk ? dwk : nullptr, 4)) return DFSS_ERR_SHAPE;
+    if (wq || wk) {
+        if (!ws) return DFSS_ERR_NULL;
+        if ((reinterpret_cast<uintptr_t>(ws) & (kAlign - 1)) != 0) return DFSS_ERR_SHAPE;
+        if (ws_bytes < dfss_qk_norm_workspace_bytes(s)) return DFSS_ERR_WORKSPACE;
+    }
+    return hip_status(dfss::launch_norm_rotate_grad(N.grad[0], N.grad[1], N.in[0], N.in[1], wq, wk, eps, N.rotary, s->B, s->Lq,
+                                                    s->d, N.f32, N.out[0], N.out[1], (float *)dwq, (float *)dwk, (float *)ws,
+                                                    (hipStream_t)stream));
+}
+
+dfss_status dfss_cache_append(const dfss_rows *K, const dfss_rows *V, int32_t rows, const int32_t *cu,
+                              const dfss_cache *cache, const void *w, const dfss_rotary *rotary, const dfss_shape *s,
+                              float eps, void *stream) {
+    dfss::PagedCache C;
+    dfss::HeadRows k, v;
+    dfss::RotaryTable rt;
+    if (!K || !V) return DFSS_ERR_NULL;
+    if (dfss_status st = cache_of(cache, s, &C)) return st;
+    if (bad_eps(eps)) return DFSS_ERR_UNSUPPORTED;
+    if (dfss_status st = rows_of(K, 2, &k)) return st;
+    if (dfss_status st = rows_of(V, 2, &v)) return st;
+    if (dfss_status st = rotary_of(rotary, s->d, &rt)) return st;
+    if (rows <= 0 || rows > (1 << 27) || s->H != C.Hk || k.H != C.Hk || v.H != C.Hk || misaligned(w) || misaligned_to(cu, 4)) return DFSS_ERR_SHAPE;
+    if (!cu && (long long)s->B * s->Lq != rows) return DFSS_ERR_SHAPE;
+    return hip_status(dfss::launch_cache_append(k, v, rows, cu, s->B, s->Lq, s->Lk, s->d, w, eps, rt, C, (hipStream_t)stream));
+}
+
+size_t dfss_cached_workspace_bytes(const dfss_shape *s, const dfss_cache *cache) {
+    dfss::PagedCache C;
+    if (cache_of(cache, s, &C) != DFSS_OK || cached_sizes(s, C.Hk) != DFSS_OK) return 0;
+    return align_up(dfss::cached_workspace_bytes(s->B, s->H, C.Hk, s->Lq, s->Lk, s->d));
+}
+
+dfss_status dfss_attention_cached(const dfss_rows *Q, int32_t rows, const int32_t *cu, const dfss_cache *cache,
+                                  const dfss_shape *s, float scale, int32_t causal, void *O, void *ws, size_t ws_bytes,
+                                  void *stream) {
+    return attention_cached(Q, rows, cu, cache, s, false, scale, causal, O, ws, ws_bytes, stream);
+}
+
+dfss_status dense_attention_cached(const dfss_rows *Q, int32_t rows, const int32_t *cu, const dfss_cache *cache,
+                                   const dfss_shape *s, float scale, int32_t causal, void *O, void *ws, size_t ws_bytes,
+                                   void *stream) {
+    return attention_cached(Q, rows, cu, cache, s, true, scale, causal, O, ws, ws_bytes, stream);
 }
 
 const char *dfss_status_string(dfss_status st) {

@@ -129,4 +129,46 @@ hipError_t launch_fused_attention_split(const void *Q, const void *K, const void
 hipError_t launch_meta_reorder(const void *src, void *dst, int BH, int Lq, int W, bool to_canonical, bool permute,
                                hipStream_t st);
 
+// Rows of H heads, d elements each, at data + b * batch + t * token + h * head (in elements; dfss_rows).
+struct HeadRows {
+    void *data;
+    long batch, token, head;
+    int H;
+};
+// The rotation's table and the tokens' positions (dfss_rotary); rot = 0: no rotation.
+struct RotaryTable {
+    const float *cos, *sin;
+    const int *pos;
+    int n_pos, rot, interleaved;
+    // position of a token, within the table whatever the array holds: pos[i], or `otherwise` without the array
+    __device__ __forceinline__ long at(long i, long otherwise) const {
+        if (rot == 0) return 0;
+        const long p = pos ? pos[i] : otherwise;
+        return p < 0 ? 0 : p < n_pos ? p : n_pos - 1;
+    }
+};
+// The paged cache of 8 bits (dfss_cache): e4m3 codes [n_pages, Hk, page, d], a power of two for each page and head, the
+// sequences' pages [B, width] and lengths [B].  page = 1 << page_shift.
+struct PagedCache {
+    uint8_t *k, *v;
+    float *k_scale, *v_scale;
+    const int *table, *len;
+    int n_pages, Hk, page_shift, width;
+};
+// Norm (weights wq, wk; null: none) and rotation of the heads of Q and K (K.H may be 0), and the gradients: part has
+// norm_rotate_workspace_bytes (not needed without weights).
+hipError_t launch_norm_rotate(const HeadRows &Q, const HeadRows &K, const void *wq, const void *wk, float eps, const RotaryTable &rt,
+                              long B, int L, int d, bool f32, const HeadRows &Qo, const HeadRows &Ko, hipStream_t st);
+size_t norm_rotate_workspace_bytes(int d);
+hipError_t launch_norm_rotate_grad(const HeadRows &dQo, const HeadRows &dKo, const HeadRows &Q, const HeadRows &K, const void *wq,
+                                   const void *wk, float eps, const RotaryTable &rt, long B, int L, int d, bool f32,
+                                   const HeadRows &dQ, const HeadRows &dK, float *dwq, float *dwk, float *part, hipStream_t st);
+// New tokens (rows of K and V, cu[b] .. cu[b + 1] - 1 for sequence b, or `most` each without cu) into the cache.
+hipError_t launch_cache_append(const HeadRows &K, const HeadRows &V, int T, const int *cu, int B, int most, int max_len, int d,
+                               const void *w, float eps, const RotaryTable &rt, const PagedCache &c, hipStream_t st);
+// Attention over the cache.  mode: 0 = 2:4, 1 = 1:2, 2 = dense; part: cached_workspace_bytes (may be 0).
+size_t cached_workspace_bytes(int B, int Hq, int Hk, int most, int max_len, int d);
+hipError_t launch_attention_cached(const HeadRows &Q, int T, const int *cu, int B, int most, int max_len, int d, int mode,
+                                   float scale, bool causal, const PagedCache &c, void *O, void *part, hipStream_t st);
+
 }  // namespace dfss

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass, fields
 from functools import cached_property
 
@@ -56,23 +57,16 @@ class _CShape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("B", "H", "Lq", "Lk", "d", "N", "M", "dtype")]
 
 
-class _CRows(ctypes.Structure):
-    _fields_ = [("data", ctypes.c_void_p), ("H", ctypes.c_int32)] + [(n, ctypes.c_int64) for n in ("batch", "token", "head")]
-
-
-class _CRotary(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_void_p) for n in ("cos", "sin", "pos")] + [(n, ctypes.c_int32) for n in ("n_pos", "rot", "interleaved")]
-
-
-class _CCache(ctypes.Structure):
-    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "table", "len")] + \
-               [(n, ctypes.c_int32) for n in ("n_pages", "Hk", "page", "width")]
+# dfss_rows, dfss_rotary, dfss_cache as bytes (a ctypes structure takes 2 us to fill, more than the checks of its tensors)
+_ROWS = struct.Struct("@Piqqq")
+_ROTARY = struct.Struct("@PPPiii")
+_CACHE = struct.Struct("@PPPPPPiiii")
 
 
 class _Call:
     """Element types, sizes and the C structure of a shape, as the calls use them.  (Deriving them on every call took 4 of
     the 11 us of host time of a small one, as much as the kernel launch itself.)"""
-    __slots__ = ("c", "ref", "torch_dtype", "O_shape", "q_numel", "kv_numel", "ragged_ws")
+    __slots__ = ("c", "ref", "torch_dtype", "O_shape", "q_numel", "kv_numel", "ragged_ws", "cached_ws")
 
     def __init__(self, s: Shape):
         self.c = s.c()
@@ -82,6 +76,7 @@ class _Call:
         self.q_numel = s.BH * s.Lq * s.d
         self.kv_numel = s.BH * s.Lk * s.d
         self.ragged_ws = None               # workspace bytes of dfss_attention_ragged, asked for once
+        self.cached_ws = {}                 # ... of the calls over a cache, by its heads
 
 
 @dataclass(frozen=True)
@@ -199,7 +194,7 @@ def load_library():
         L.dfss_attention_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, sp, f32, vp, vp, vp, vp, sz, vp]
         L.dfss_meta_to_canonical.argtypes = [vp, sp, vp, vp]
         L.dfss_meta_from_canonical.argtypes = [vp, sp, vp, vp]
-        rows, rot, cache = (ctypes.POINTER(c) for c in (_CRows, _CRotary, _CCache))
+        rows = rot = cache = vp     # (given as bytes)
         n32 = ctypes.c_int32
         L.dfss_qk_norm_rotate.argtypes = [rows, rows, vp, vp, rot, sp, f32, rows, rows, vp]
         L.dfss_qk_norm_workspace_bytes.argtypes = [sp]
@@ -783,35 +778,39 @@ def dfss_meta_from_canonical(canon, s: Shape, meta=None):
 # ---- around a decoder's attention ------------------------------------------------------------------------------
 
 
-def _device(t: torch.Tensor, dtype, what: str) -> int:
-    """Pointer of a tensor of the given type (or one of several) on the current device."""
+def _current(device: int) -> bool:
+    """Whether that is the current device (-1: the host's)."""
+    return device >= 0 and device == torch._C._cuda_getDevice()
+
+
+def _array(t: torch.Tensor, dtype, shape, device: int | None, what: str) -> int:
+    """Pointer of a contiguous tensor of the given type (or of one of several) and shape, on the current device, or on the
+    given one, which is known to be that."""
+    there = t.get_device()
+    if t.dtype is dtype and t.shape == shape and (there == device or device is None and _current(there)) and t.is_contiguous():
+        return t.data_ptr()
     if t.dtype is not dtype and not (isinstance(dtype, tuple) and t.dtype in dtype):
         raise ValueError(f"{what}: expected {dtype}, got {t.dtype}")
-    if not t.is_cuda or t.device.index != torch._C._cuda_getDevice():
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous tensor {list(shape)}, got {list(t.shape)}")
+    if not _current(there):
         raise ValueError(f"{what}: expected a tensor on the current device, got one on {t.device}")
     return t.data_ptr()
-
-
-def _array(t: torch.Tensor, dtype, shape, what: str) -> int:
-    """The same of a contiguous one of the given shape."""
-    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise ValueError(f"{what}: expected a contiguous tensor {list(shape)}, got {list(t.shape)}")
-    return _device(t, dtype, what)
 
 
 class Rotary:
     """Rotary positions (``dfss_rotary``): cos, sin float32 [n_pos, rot/2]; pos int32, the position of every token of a
     call (None: its place in its sequence); pairs (i, i + rot/2), or neighbours if ``interleaved``.  Keeps its tensors."""
-    __slots__ = ("cos", "sin", "pos", "interleaved", "_c", "_ref")
+    __slots__ = ("cos", "sin", "pos", "interleaved", "device", "_c")
 
     def __init__(self, cos, sin, pos=None, interleaved: bool = False):
-        if cos.dim() != 2:
-            raise ValueError(f"cos, sin: expected [n_pos, rot/2], got {list(cos.shape)}")
+        shape, f = cos.shape, torch.float32
+        if len(shape) != 2:
+            raise ValueError(f"cos, sin: expected [n_pos, rot/2], got {list(shape)}")
         self.cos, self.sin, self.pos, self.interleaved = cos, sin, pos, interleaved
-        self._c = _CRotary(_array(cos, torch.float32, cos.shape, "cos"), _array(sin, torch.float32, cos.shape, "sin"),
-                           None if pos is None else _array(pos, torch.int32, pos.shape, "pos"),
-                           cos.shape[0], 2 * cos.shape[1], int(bool(interleaved)))
-        self._ref = ctypes.byref(self._c)
+        p, self.device = _array(cos, f, shape, None, "cos"), cos.get_device()
+        self._c = _ROTARY.pack(p, _array(sin, f, shape, self.device, "sin"),
+                               0 if pos is None else _array(pos, torch.int32, pos.shape, self.device, "pos"), shape[0], 2 * shape[1], bool(interleaved))
 
 
 def _rotary(r: Rotary | None, tokens: int):
@@ -819,54 +818,71 @@ def _rotary(r: Rotary | None, tokens: int):
         return None
     if r.pos is not None and r.pos.numel() != tokens:
         raise ValueError(f"pos: expected {tokens} positions, got {r.pos.numel()}")
-    return r._ref
+    if not _current(r.device):
+        raise ValueError(f"rotary: expected one on the current device, got one on {r.cos.device}")
+    return r._c
+
+
+_CODES = (torch.uint8, torch.float8_e4m3fn)
 
 
 class Cache:
     """A paged cache of 8 bits (``dfss_cache``): k, v uint8 or float8_e4m3fn [n_pages, Hk, page, d], their scales float32
     [n_pages, Hk], table int32 [B, width], len int32 [B].  Keeps its tensors."""
-    __slots__ = ("k", "v", "k_scale", "v_scale", "table", "len", "_c", "_ref")
+    __slots__ = ("k", "v", "k_scale", "v_scale", "table", "len", "B", "Hk", "d", "device", "_c")
 
     def __init__(self, k, v, k_scale, v_scale, table, len):
+        shape, where, f, i = k.shape, table.shape, torch.float32, torch.int32
         if k.dim() != 4 or table.dim() != 2:
-            raise ValueError(f"expected k, v [n_pages, Hk, page, d] and table [B, width], got {list(k.shape)}, {list(table.shape)}")
+            raise ValueError(f"expected k, v [n_pages, Hk, page, d] and table [B, width], got {list(shape)}, {list(where)}")
         self.k, self.v, self.k_scale, self.v_scale, self.table, self.len = k, v, k_scale, v_scale, table, len
-        codes = (torch.uint8, torch.float8_e4m3fn)
-        self._c = _CCache(_array(k, codes, k.shape, "k"), _array(v, codes, k.shape, "v"),
-                          _array(k_scale, torch.float32, k.shape[:2], "k_scale"), _array(v_scale, torch.float32, k.shape[:2], "v_scale"),
-                          _array(table, torch.int32, table.shape, "table"), _array(len, torch.int32, table.shape[:1], "len"),
-                          k.shape[0], k.shape[1], k.shape[2], table.shape[1])
-        self._ref = ctypes.byref(self._c)
+        n, self.Hk, page, self.d = shape
+        self.B, width = where
+        scales, codes = (n, self.Hk), k.dtype if k.dtype in _CODES else _CODES
+        p, dev = _array(k, codes, shape, None, "k"), k.get_device()
+        self.device = dev
+        self._c = _CACHE.pack(p, _array(v, codes, shape, dev, "v"), _array(k_scale, f, scales, dev, "k_scale"),
+                              _array(v_scale, f, scales, dev, "v_scale"), _array(table, i, where, dev, "table"),
+                              _array(len, i, where[:1], dev, "len"), n, self.Hk, page, width)
 
 
 def _rows(t: torch.Tensor | None, shape, dtype, what: str, out: bool = False):
-    """Rows of heads.  [batch, token, head, d] with any strides of the first three, or, for shape[0] * heads rows of a batch
-    element each, the contiguous [batch * head, token, d] of the attention calls; [token, head, d] where shape has no batch.
-    shape: (batch, token, d) or (token, d)."""
+    """Rows of heads, as bytes, and their number of heads (None, 0 without a tensor): [batch, token, head, d] with any strides of the first
+    three, or the contiguous [batch * head, token, d] of the attention calls, for a shape (batch, token, d); [token, head, d]
+    with any strides of the first two for a shape (token, d)."""
     if t is None:
-        return None
-    p, n, x = _device(t, dtype, what), t.shape, t.stride()
-    d = shape[-1]
+        return None, 0
+    if t.dtype is not dtype:
+        raise ValueError(f"{what}: expected {dtype}, got {t.dtype}")
+    n, x, d, dims = t.shape, t.stride(), shape[-1], t.dim()
     if len(shape) == 2:
-        if t.dim() != 3 or n[0] != shape[0] or n[2] != d or x[2] != 1:
+        if dims != 3 or n[0] != shape[0] or n[2] != d or x[2] != 1:
             raise ValueError(f"{what}: expected [{shape[0]}, heads, {d}] with elements side by side, got {list(n)}")
         H, batch, token, head = n[1], 0, x[0] if n[0] > 1 else 0, x[1] if n[1] > 1 else 0
-    elif t.dim() == 3:
+    elif dims == 3:
         if n[0] % shape[0] or n[1] != shape[1] or n[2] != d or not t.is_contiguous():
             raise ValueError(f"{what}: expected a contiguous [{shape[0]} * heads, {shape[1]}, {d}], got {list(n)}")
         H = n[0] // shape[0]
         batch, token, head = H * shape[1] * d, d, shape[1] * d
     else:
-        if t.dim() != 4 or n[0] != shape[0] or n[1] != shape[1] or n[3] != d or x[3] != 1:
+        if dims != 4 or n[0] != shape[0] or n[1] != shape[1] or n[3] != d or x[3] != 1:
             raise ValueError(f"{what}: expected [{shape[0]}, {shape[1]}, heads, {d}] with elements side by side, got {list(n)}")
         H, batch, token, head = n[2], x[0] if n[0] > 1 else 0, x[1] if n[1] > 1 else 0, x[2] if n[2] > 1 else 0
-    if out and any(k > 1 and y == 0 for k, y in zip(n, x)):
+    if out and 0 in x and any(k > 1 and y == 0 for k, y in zip(n, x)):
         raise ValueError(f"{what}: a result cannot share rows")
-    return _CRows(p, H, batch, token, head)
+    if not _current(t.get_device()):
+        raise ValueError(f"{what}: expected a tensor on the current device, got one on {t.device}")
+    return _ROWS.pack(t.data_ptr(), H, batch, token, head), H
+
+
+def _headed(B: int, H: int, L: int, d: int, dtype, device):
+    """A new [B * H, L, d] and its rows, as _rows gives them."""
+    t = torch.empty((B * H, L, d), dtype=dtype, device=device)
+    return t, _ROWS.pack(t.data_ptr(), H, H * L * d, d, L * d)
 
 
 def _weight(w: torch.Tensor | None, dtype, d: int, what: str):
-    return None if w is None else _array(w, dtype, (d,), what)
+    return None if w is None else _array(w, dtype, (d,), None, what)
 
 
 def dfss_qk_norm_rotate(Q, K, wq, wk, rotary: Rotary | None, s: Shape, eps: float = 1e-6, Qo=None, Ko=None):
@@ -874,14 +890,17 @@ def dfss_qk_norm_rotate(Q, K, wq, wk, rotary: Rotary | None, s: Shape, eps: floa
     Q, K: [B, Lq, heads, d] with any strides (or [B * heads, Lq, d]); K may be None.  Returns Qo, Ko, [B * heads, Lq, d] as
     the attention calls take them unless given."""
     t, shape = s._call.torch_dtype, (s.B, s.Lq, s.d)
-    q, k = _rows(Q, shape, t, "Q"), _rows(K, shape, t, "K")
+    (q, Hq), (k, Hk) = _rows(Q, shape, t, "Q"), _rows(K, shape, t, "K")
     if Qo is None:
-        Qo = torch.empty((s.B * q.H, s.Lq, s.d), dtype=t, device=Q.device)
+        Qo, qo = _headed(s.B, Hq, s.Lq, s.d, t, Q.device)
+    else:
+        qo = _rows(Qo, shape, t, "Qo", True)[0]
     if Ko is None and K is not None:
-        Ko = torch.empty((s.B * k.H, s.Lq, s.d), dtype=t, device=Q.device)
+        Ko, ko = _headed(s.B, Hk, s.Lq, s.d, t, Q.device)
+    else:
+        ko = _rows(Ko, shape, t, "Ko", True)[0]
     st = load_library().dfss_qk_norm_rotate(q, k, _weight(wq, t, s.d, "wq"), _weight(wk, t, s.d, "wk"),
-                                            _rotary(rotary, s.B * s.Lq), s._call.ref, eps, _rows(Qo, shape, t, "Qo", True),
-                                            _rows(Ko, shape, t, "Ko", True), _stream())
+                                            _rotary(rotary, s.B * s.Lq), s._call.ref, eps, qo, ko, _stream())
     _check("dfss_qk_norm_rotate", st)
     return Qo, Ko
 
@@ -895,11 +914,11 @@ def dfss_qk_norm_rotate_backward(dQo, dKo, Q, K, wq, wk, rotary: Rotary | None, 
     """Gradients of dfss_qk_norm_rotate: (dQ, dK, dwq, dwk), those of Q and K [B, Lq, heads, d] unless given, those of the
     weights float32 [d] (None where there is no weight)."""
     t, shape = s._call.torch_dtype, (s.B, s.Lq, s.d)
-    q, k = _rows(Q, shape, t, "Q"), _rows(K, shape, t, "K")
+    (q, Hq), (k, Hk) = _rows(Q, shape, t, "Q"), _rows(K, shape, t, "K")
     if dQ is None:
-        dQ = torch.empty((s.B, s.Lq, q.H, s.d), dtype=t, device=Q.device)
+        dQ = torch.empty((s.B, s.Lq, Hq, s.d), dtype=t, device=Q.device)
     if dK is None and K is not None:
-        dK = torch.empty((s.B, s.Lq, k.H, s.d), dtype=t, device=Q.device)
+        dK = torch.empty((s.B, s.Lq, Hk, s.d), dtype=t, device=Q.device)
     if dwq is None and wq is not None:
         dwq = torch.empty(s.d, dtype=torch.float32, device=Q.device)
     if dwk is None and wk is not None and K is not None:
@@ -907,8 +926,8 @@ def dfss_qk_norm_rotate_backward(dQo, dKo, Q, K, wq, wk, rotary: Rotary | None, 
     if ws is None and (dwq is not None or dwk is not None):
         ws = _alloc_bytes(dfss_qk_norm_workspace_bytes(s), Q.device)
     st = load_library().dfss_qk_norm_rotate_backward(
-        _rows(dQo, shape, t, "dQo"), _rows(dKo, shape, t, "dKo"), q, k, _weight(wq, t, s.d, "wq"), _weight(wk, t, s.d, "wk"),
-        _rotary(rotary, s.B * s.Lq), s._call.ref, eps, _rows(dQ, shape, t, "dQ", True), _rows(dK, shape, t, "dK", True),
+        _rows(dQo, shape, t, "dQo")[0], _rows(dKo, shape, t, "dKo")[0], q, k, _weight(wq, t, s.d, "wq"), _weight(wk, t, s.d, "wk"),
+        _rotary(rotary, s.B * s.Lq), s._call.ref, eps, _rows(dQ, shape, t, "dQ", True)[0], _rows(dK, shape, t, "dK", True)[0],
         _weight(dwq, torch.float32, s.d, "dwq"), _weight(dwk, torch.float32, s.d, "dwk"), _ptr(ws),
         0 if ws is None else ws.numel() * ws.element_size(), _stream())
     _check("dfss_qk_norm_rotate_backward", st)
@@ -916,15 +935,15 @@ def dfss_qk_norm_rotate_backward(dQo, dKo, Q, K, wq, wk, rotary: Rotary | None, 
 
 
 def _offsets(cu: torch.Tensor | None, s: Shape):
-    return None if cu is None else _array(cu, torch.int32, (s.B + 1,), "cu")
+    return None if cu is None else _array(cu, torch.int32, (s.B + 1,), None, "cu")
 
 
 def _cache(c: Cache, s: Shape):
-    if c.table.shape[0] != s.B or c.k.shape[3] != s.d:
-        raise ValueError(f"cache: expected {s.B} sequences and head size {s.d}, got {c.table.shape[0]} and {c.k.shape[3]}")
-    if c.k.device.index != torch._C._cuda_getDevice():
+    if c.B != s.B or c.d != s.d:
+        raise ValueError(f"cache: expected {s.B} sequences and head size {s.d}, got {c.B} and {c.d}")
+    if not _current(c.device):
         raise ValueError(f"cache: expected one on the current device, got one on {c.k.device}")
-    return c._ref
+    return c._c
 
 
 def dfss_cache_append(K, V, cu, cache: Cache, w, rotary: Rotary | None, s: Shape, eps: float = 1e-6):
@@ -932,28 +951,37 @@ def dfss_cache_append(K, V, cu, cache: Cache, w, rotary: Rotary | None, s: Shape
     sequence b (cu None: Lq each); cache.len holds the lengths with them.  Keys are normed (w None: not) and rotated on
     the way.  s: B sequences, H = Hk key heads, at most Lk tokens a sequence."""
     n = K.shape[0]
-    st = load_library().dfss_cache_append(_rows(K, (n, s.d), torch.bfloat16, "K"), _rows(V, (n, s.d), torch.bfloat16, "V"), n,
+    st = load_library().dfss_cache_append(_rows(K, (n, s.d), torch.bfloat16, "K")[0], _rows(V, (n, s.d), torch.bfloat16, "V")[0], n,
                                           _offsets(cu, s), _cache(cache, s), _weight(w, torch.bfloat16, s.d, "w"),
                                           _rotary(rotary, n), s._call.ref, eps, _stream())
     _check("dfss_cache_append", st)
 
 
 def dfss_cached_workspace_bytes(s: Shape, cache: Cache) -> int:
-    return int(load_library().dfss_cached_workspace_bytes(s._call.ref, cache._ref))
+    return int(load_library().dfss_cached_workspace_bytes(s._call.ref, cache._c))
 
 
 def _attention_cached(name: str, Q, cu, cache: Cache, s: Shape, scale: float, causal: bool, O, ws):
     n = Q.shape[0]
-    q, c = _rows(Q, (n, s.d), torch.bfloat16, "Q"), _cache(cache, s)
+    (q, H), c = _rows(Q, (n, s.d), torch.bfloat16, "Q"), _cache(cache, s)
     if O is None:
-        O = torch.empty((n, q.H, s.d), dtype=torch.bfloat16, device=Q.device)
+        O = torch.empty((n, H, s.d), dtype=torch.bfloat16, device=Q.device)
+        o = O.data_ptr()
+    else:
+        o = _array(O, torch.bfloat16, (n, H, s.d), None, "O")
     L = load_library()
-    if ws is None:
-        need = L.dfss_cached_workspace_bytes(s._call.ref, c)
-        ws = _alloc_bytes(need, Q.device) if need else None
-    st = getattr(L, name)(q, n, _offsets(cu, s), c, s._call.ref, scale, int(bool(causal)),
-                          _array(O, torch.bfloat16, (n, q.H, s.d), "O"), _ptr(ws),
-                          0 if ws is None else ws.numel() * ws.element_size(), _stream())
+    w = None
+    if ws is not None:
+        need, w = ws.numel() * ws.element_size(), _ptr(ws)
+    else:
+        need = s._call.cached_ws.get(cache.Hk)      # (of a valid shape it depends on nothing else of the cache)
+        if not need:
+            need = s._call.cached_ws[cache.Hk] = L.dfss_cached_workspace_bytes(s._call.ref, c)
+        if need:
+            ws = _alloc_bytes(need, Q.device)
+            w = ws.data_ptr()
+    st = getattr(L, name)(q, n, None if cu is None else _array(cu, torch.int32, (s.B + 1,), None, "cu"), c, s._call.ref, scale,
+                          1 if causal else 0, o, w, need, _stream())
     _check(name, st)
     return O
 

@@ -31,11 +31,76 @@ constexpr int KB = 64;    // keys per block
 constexpr float kTau = 8.0f * 1.4426950408889634f;   // how far (in exponents of two) scores may exceed the reference
 enum { MODE_2TO4 = 0, MODE_1TO2 = 1, MODE_DENSE = 2 };
 
+// A load at an address that is the same in every lane, of memory that no kernel of the call writes, by the scalar unit: what
+// follows from it (pages, addresses) stays off the vector unit.
+template <typename T>
+__device__ __forceinline__ T scalar_load(const T *p, long i) {
+    typedef const T __attribute__((address_space(4))) *constant;
+    return ((constant)(uintptr_t)p)[i];
+}
+
+// Integer division is vector work, and so would be all that follows from its result.
+__device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 struct Sizes {
-    int T, B, Hq, G, most, max_len, tiles, splits, least;   // tiles: row tiles (of 16 RT rows) of a sequence and key head
+    int T, B, Hq, G, most, max_len, tiles, target, least;   // tiles: row tiles (of 16 RT rows) of a sequence and key head
     long q_token, q_head;
+    double per_target;   // 1 / target
     float c;          // scale * log2(e)
     int causal;
+};
+
+// Where keys are shared: sequences are cut into shares of `per` blocks, the same for all of them, so that each of `target`
+// workgroups for every key head and row tile gets about one, whatever the lengths are: per = ceil(all blocks / target), so that all
+// sequences together have at most target + B shares.  They are numbered through the sequences.
+struct Shares {
+    int per;
+    // Blocks of a sequence by its length (its row tiles may see fewer under the causal mask).
+    static __device__ __forceinline__ int blocks(const Sizes &s, const PagedCache &c, int b) {
+        const long capacity = (long)c.width << c.page_shift;
+        const int most = s.max_len < capacity ? s.max_len : (int)capacity, len = c.len[b];
+        return ((len < 0 ? 0 : len < most ? len : most) + KB - 1) / KB;
+    }
+    // Sum over the lanes up to this one.
+    static __device__ __forceinline__ int scan(int x) {
+#define DFSS_STEP(ctrl, rows) x += __builtin_amdgcn_update_dpp(0, x, ctrl, rows, 0xF, true)
+        DFSS_STEP(0x111, 0xF);   // from 1, 2, 4 and 8 lanes before, within rows of 16
+        DFSS_STEP(0x112, 0xF);
+        DFSS_STEP(0x114, 0xF);
+        DFSS_STEP(0x118, 0xF);
+        DFSS_STEP(0x142, 0xA);   // the last lane of the row before into rows 1 and 3
+        DFSS_STEP(0x143, 0xC);   // lane 31 into rows 2 and 3
+#undef DFSS_STEP
+        return x;
+    }
+    __device__ __forceinline__ void init(const Sizes &s, const PagedCache &c, int l) {
+        int total = 0;   // (plan: at most 2^30 blocks)
+        for (int i = 0; i < s.B; i += 64) total += i + l < s.B ? blocks(s, c, i + l) : 0;
+        total = __builtin_amdgcn_readlane(scan(total), 63);
+        int p = (int)((double)total * s.per_target);
+        p += (long)p * s.target < total;   // rounded up (a division would take ten times the instructions)
+        per = scalar(p < s.least ? s.least : p);
+    }
+    // Number of the first share of sequence `upto`, or (upto < 0) the sequence that share `at` belongs to, and the number of
+    // its first one.  Returns -1 if there is no such share.
+    __device__ __forceinline__ int find(const Sizes &s, const PagedCache &c, int l, int at, int upto, int *first) const {
+        int before = 0;
+        for (int i = 0; i < s.B; i += 64) {
+            const int n = i + l < s.B ? (blocks(s, c, i + l) + per - 1) / per : 0, sum = scan(n);
+            if (upto >= 0) {
+                if (upto < i + 64) return before + __builtin_amdgcn_readlane(sum - n, upto - i);
+            } else {
+                const uint64_t after = __ballot(at < before + sum);
+                if (after) {
+                    const int lane = __builtin_ctzll(after);
+                    *first = before + __builtin_amdgcn_readlane(sum - n, lane);
+                    return i + lane;
+                }
+            }
+            before += __builtin_amdgcn_readlane(sum, 63);
+        }
+        return upto >= 0 ? before : -1;
+    }
 };
 
 // What a row tile needs to know of its sequence.
@@ -43,12 +108,11 @@ struct Rows {
     int b, h, lo, n, len, first;   // first: position of query 0
     int r0, rows;                  // first row of the tile, rows of the sequence
     int keys;                      // keys that any row of the tile sees
-    __device__ __forceinline__ bool init(const Sizes &s, const int *cu, const PagedCache &c, int item, int tile_rows) {
-        const int tile = item % s.tiles, bh = item / s.tiles;
-        b = bh / c.Hk, h = bh - b * c.Hk;
+    __device__ __forceinline__ bool init(const Sizes &s, const int *cu, const PagedCache &c, int seq, int head, int tile, int tile_rows) {
+        b = seq, h = head;
         lo = b * s.most, n = s.most;
         if (cu) {
-            lo = cu[b], n = cu[b + 1];
+            lo = scalar_load(cu, b), n = scalar_load(cu, b + 1);
             lo = lo < 0 ? 0 : lo < s.T ? lo : s.T;
             n = n < lo ? 0 : (n < s.T ? n : s.T) - lo;
         }
@@ -56,12 +120,13 @@ struct Rows {
         r0 = tile * tile_rows, rows = queries * s.G;
         if (r0 >= rows) return false;
         const long capacity = (long)c.width << c.page_shift;
-        len = c.len[b] < 0 ? 0 : c.len[b];
+        len = scalar_load(c.len, b);
+        len = len < 0 ? 0 : len;
         first = len - n;           // (by the length given: a longer one than the call allows is cut, positions stay)
         const int most_keys = s.max_len < capacity ? s.max_len : (int)capacity;
         len = len < most_keys ? len : most_keys;
         const int last = r0 + tile_rows < rows ? r0 + tile_rows - 1 : rows - 1;
-        keys = limit(s, last);
+        keys = scalar(limit(s, last));
         return true;
     }
     // keys that row r sees: those before it
@@ -71,18 +136,14 @@ struct Rows {
         return x < 0 ? 0 : x < len ? x : len;
     }
     __device__ __forceinline__ int blocks() const { return (keys + KB - 1) / KB; }
-    // blocks of one of the workgroups that share the keys: the more the fewer of them there are
-    __device__ __forceinline__ int per_split(const Sizes &s) const {
-        const int per = (blocks() + s.splits - 1) / s.splits;
-        return per < s.least ? s.least : per;
-    }
 };
 
 template <int D>
 constexpr int partial_floats() { return 16 * (D + 2); }   // of a 16-row tile: references, sums, O
 
-template <int D, int MODE, int NW, int RT, bool SPLIT>
-__global__ __launch_bounds__(64 * NW) void k_cached(const __bf16 *__restrict__ Q, const int *__restrict__ cu, PagedCache cache,
+// BIG: pages of 64 tokens or more, a block lies in one.
+template <int D, int MODE, int NW, int RT, bool BIG>
+__global__ __launch_bounds__(64 * NW, RT == 1 && D == 64 ? 3 : RT <= 2 ? 2 : 1) void k_cached(const __bf16 *__restrict__ Q, const int *__restrict__ cu, PagedCache cache,
                                                     const uint8_t *__restrict__ Kc, const uint8_t *__restrict__ Vc,
                                                     const float *__restrict__ Ks, const float *__restrict__ Vs,
                                                     const int *__restrict__ table, Sizes sz, uint16_t *__restrict__ O,
@@ -93,22 +154,32 @@ __global__ __launch_bounds__(64 * NW) void k_cached(const __bf16 *__restrict__ Q
     constexpr int VW = D / 64;          // dwords of V that a lane holds of a key
     constexpr int NF = 4 * DT + 5;      // floats per lane of a partial result
     constexpr bool DENSE = MODE == MODE_DENSE;
-    constexpr int KG = DENSE ? 2 : 1;   // 16-key groups that the lane's K rows lie in
     __shared__ float slots[NW * NF * 64];
 
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = threadIdx.x & 63, li = l & 15, kb = l >> 4;
-    const unsigned share = xcd_contiguous(blockIdx.x, gridDim.x);
-    const unsigned item = SPLIT ? share / (unsigned)sz.splits : share;
-    const int sp = SPLIT ? share % (unsigned)sz.splits : 0;
+    // workgroups: [sequence][head][tile], or [share][head][tile] where keys are shared
+    const unsigned id = xcd_contiguous(blockIdx.x, gridDim.x);
+    const int x = scalar(id / (unsigned)sz.tiles), tile = id - x * sz.tiles, number = scalar(x / (unsigned)cache.Hk), head = x - number * cache.Hk;
+    int seq = number, begin = 0, end, first = 0;
+    Shares sh;
+    if (sz.target) {
+        sh.init(sz, cache, l);
+        seq = sh.find(sz, cache, l, number, -1, &first);
+        if (seq < 0) return;
+    }
     Rows R;
-    if (!R.init(sz, cu, cache, item, 16 * RT)) return;
+    if (!R.init(sz, cu, cache, seq, head, tile, 16 * RT)) return;
     const int nblocks = R.blocks();
-    const int per = SPLIT ? R.per_split(sz) : nblocks;
-    const int begin = sp * per, end = begin + per < nblocks ? begin + per : nblocks;
-    if (SPLIT && begin >= nblocks) return;
+    end = nblocks;
+    if (sz.target) {
+        begin = (number - first) * sh.per;
+        if (begin >= nblocks) return;
+        end = begin + sh.per < nblocks ? begin + sh.per : nblocks;
+    }
+    const bool alone = begin == 0 && end == nblocks;   // nobody else has keys of these rows: no second kernel
     const int page_mask = (1 << cache.page_shift) - 1, last_entry = (R.keys > 0 ? R.keys - 1 : 0) >> cache.page_shift;
     const int *const my_table = table + (long)R.b * cache.width;
-    const int seen_by_all = R.limit(sz, R.r0);
+    const int seen_by_all = scalar(R.limit(sz, R.r0));
 
     // Q operand of step s: lane (column li, chunk kb) holds the elements 64 (s / 2) + 16 kb + 8 (s % 2) .. +7
     bf16x8 bq[RT][STEPS];
@@ -127,61 +198,82 @@ __global__ __launch_bounds__(64 * NW) void k_cached(const __bf16 *__restrict__ Q
     // Key of MFMA row i of tile t, so that a lane (query li, kb) ends up with whole runs and, for the second product,
     //   pruned  keys 16 kb .. +15                 row i: key 16 (i / 4) + 4 t + i % 4
     //   full    keys 8 kb .. +7 and 32 + the same  row i: key 32 (t / 2) + 8 (i / 4) + 4 (t % 2) + i % 4
-    struct Block {
-        u32x4 k[4][SS];
-        uint32_t v[2][8][VW];
-        float ks[KG], vs[2];
-        int bad;          // groups of 16 keys whose page is none (a bit each)
+    // A block is NG groups of keys, each in one page (16 keys, or all 64).  Pages and scales are the same for the whole wave
+    // (scalar loads): the pages two blocks ahead, the scales one.
+    constexpr int NG = BIG ? 1 : 4;
+    struct Pages {
+        int id[NG], bad;      // page of each group (0 where there is none), and a bit for each 16 keys without one
     };
-    const uint32_t k_lane = (uint32_t)((DENSE ? 8 * ((li >> 2) & 1) + (li & 3) : li & 3) * D + 16 * kb);
-    const uint32_t v_lane = (uint32_t)(8 * (kb & 1) * D + li * (4 * VW));
-    auto load_block = [&](int jb, Block &b) {
-        long at[4];
-        float ks[4], vs[4];
-        b.bad = 0;
+    struct Scales {
+        float k[NG], v[NG];
+    };
+    auto pages = [&](int jb) {
+        Pages p;
+        p.bad = 0;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int key = jb * KB + 16 * g;
-            int entry = key >> cache.page_shift;
-            entry = __builtin_amdgcn_readfirstlane(entry < last_entry ? entry : last_entry);
-            int id = my_table[entry];
-            if ((unsigned)id >= (unsigned)cache.n_pages) id = 0, b.bad |= 1 << g;
-            const long head = (long)id * cache.Hk + R.h;
-            at[g] = ((head << cache.page_shift) + (key & page_mask)) * D;
-            ks[g] = Ks[head];
-            vs[g] = Vs[head];
+        for (int g = 0; g < NG; ++g) {
+            const int entry = (jb * KB + 16 * g) >> cache.page_shift;
+            const int id = scalar_load(my_table, entry < last_entry ? entry : last_entry);
+            const bool none = (unsigned)id >= (unsigned)cache.n_pages;
+            p.id[g] = none ? 0 : id;
+            p.bad |= none ? (BIG ? 15 : 1 << g) : 0;
         }
-        const int kg = li >> 2, vg = kb >> 1;
-        long ka[KG];
-        if constexpr (DENSE) {
+        return p;
+    };
+    auto scales = [&](const Pages &p) {
+        Scales s;
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                ka[x] = li & 8 ? at[2 * x + 1] : at[2 * x];
-                b.ks[x] = li & 8 ? ks[2 * x + 1] : ks[2 * x];
-            }
-        } else {
-            const long a0 = kg & 1 ? at[1] : at[0], a1 = kg & 1 ? at[3] : at[2];
-            const float s0 = kg & 1 ? ks[1] : ks[0], s1 = kg & 1 ? ks[3] : ks[2];
-            ka[0] = kg & 2 ? a1 : a0;
-            b.ks[0] = kg & 2 ? s1 : s0;
+        for (int g = 0; g < NG; ++g) {
+            const long at = (long)p.id[g] * cache.Hk + R.h;
+            s.k[g] = scalar_load(Ks, at);
+            s.v[g] = scalar_load(Vs, at);
+        }
+        return s;
+    };
+    auto place = [&](const Pages &p, int jb, int g) {   // bytes before a group's first key
+        return ((((long)p.id[g] * cache.Hk + R.h) << cache.page_shift) + ((jb * KB + 16 * g) & page_mask)) * D;
+    };
+    auto pick = [](bool second, auto x, auto y) { return second ? y : x; };   // (by value: of an array it would be a load)
+    constexpr int G1 = BIG ? 0 : 1, G2 = BIG ? 0 : 2, G3 = BIG ? 0 : 3;
+    // first key that the lane loads, within its group: of K, and of V
+    const int k_group = DENSE ? li >> 3 : li >> 2, v_group = kb >> 1;
+    const uint32_t k_lane = (uint32_t)(((BIG ? 16 * k_group : 0) + (DENSE ? 8 * ((li >> 2) & 1) + (li & 3) : li & 3)) * D + 16 * kb);
+    const uint32_t v_lane = (uint32_t)(((BIG ? 16 * v_group : 0) + 8 * (kb & 1)) * D + li * (4 * VW));
+
+    u32x4 kr[4][SS];             // the block's K and V, as they lie in memory
+    uint32_t vr[2][8][VW];
+    auto load_k = [&](const Pages &p, int jb) {
+        long at[NG], half[2];
+#pragma unroll
+        for (int g = 0; g < NG; ++g) at[g] = place(p, jb, g);
+        half[0] = half[1] = at[0];
+        if constexpr (!BIG) {
+            half[0] = pick(k_group & 1, at[0], at[G1]), half[1] = pick(k_group & 1, at[G2], at[G3]);
+            if constexpr (!DENSE) half[0] = half[1] = pick(k_group & 2, half[0], half[1]);
         }
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            const uint8_t *const p = Kc + ka[DENSE ? t >> 1 : 0] + k_lane + (DENSE ? 4 * (t & 1) : 4 * t) * D;
+            // (DENSE: the last two tiles are those of keys 32 .. 63)
+            const uint8_t *const q = Kc + half[t >> 1] + (k_lane + (DENSE ? 4 * (t & 1) + (BIG ? 32 * (t >> 1) : 0) : 4 * t) * D);
 #pragma unroll
-            for (int x = 0; x < SS; ++x) b.k[t][x] = *reinterpret_cast<const u32x4 *>(p + 64 * x);
+            for (int x = 0; x < SS; ++x) kr[t][x] = *reinterpret_cast<const u32x4 *>(q + 64 * x);
         }
+    };
+    auto load_v = [&](const Pages &p, int jb) {
+        long at[NG];
+#pragma unroll
+        for (int g = 0; g < NG; ++g) at[g] = place(p, jb, g);
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
-            const uint8_t *const p = Vc + (vg ? at[2 * st + 1] : at[2 * st]) + v_lane;
-            b.vs[st] = vg ? vs[2 * st + 1] : vs[2 * st];
+            const long from = BIG ? at[0] : st ? pick(v_group, at[G2], at[G3]) : pick(v_group, at[0], at[G1]);
+            const uint8_t *const q = Vc + from + (v_lane + (BIG ? 32 * st * D : 0));
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 if constexpr (VW == 2) {
-                    const u32x2 x = *reinterpret_cast<const u32x2 *>(p + e * D);
-                    b.v[st][e][0] = x[0], b.v[st][e][VW - 1] = x[1];
+                    const u32x2 x = *reinterpret_cast<const u32x2 *>(q + e * D);
+                    vr[st][e][0] = x[0], vr[st][e][VW - 1] = x[1];
                 } else {
-                    b.v[st][e][0] = *reinterpret_cast<const uint32_t *>(p + e * D);
+                    vr[st][e][0] = *reinterpret_cast<const uint32_t *>(q + e * D);
                 }
             }
         }
@@ -204,19 +296,40 @@ __global__ __launch_bounds__(64 * NW) void k_cached(const __bf16 *__restrict__ Q
     constexpr std::false_type lo16{};
     constexpr std::true_type hi16{};
 
-    auto block = [&](int jb, Block &b) {
-        const bool masked = jb * KB + KB > seen_by_all || b.bad;   // (the same in every lane)
+    // A block: the scores take K out of its registers, which the next block's K then goes into; the second product takes V.
+    // So one or the other is on its way all the time, with registers for one block.
+    Pages p_now, p_next;
+    Scales sc;
+    int jb = begin + w;
+    if (jb < end) {
+        p_now = pages(jb);
+        sc = scales(p_now);
+        load_k(p_now, jb);
+        load_v(p_now, jb);
+        p_next = pages(jb + NW);
+    }
+    for (; jb < end; jb += NW) {
+        const bool more = jb + NW < end;
+        const bool masked = jb * KB + KB > seen_by_all || p_now.bad;   // (the same in every lane)
+        float k_s[2] = {sc.k[0], sc.k[0]}, v_s[2] = {sc.v[0], sc.v[0]};
+        if constexpr (!BIG) {
+            k_s[0] = pick(k_group & 1, sc.k[0], sc.k[G1]), k_s[1] = pick(k_group & 1, sc.k[G2], sc.k[G3]);
+            if constexpr (!DENSE) k_s[0] = k_s[1] = pick(k_group & 2, k_s[0], k_s[1]);
+            v_s[0] = pick(v_group, sc.v[0], sc.v[G1]), v_s[1] = pick(v_group, sc.v[G2], sc.v[G3]);
+        }
+        const int bad = p_now.bad;
+        if (more) sc = scales(p_next);
         // s[rt][t][r] = q . k of query li of tile rt and the lane's key r of tile t
         f32x4 s[RT][4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             bf16x8 a[STEPS];
-            const float ks = b.ks[DENSE ? t >> 1 : 0];
+            const float ks = k_s[t >> 1];
 #pragma unroll
             for (int x = 0; x < SS; ++x)
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    const uint32_t c0 = b.k[t][x][2 * y], c1 = b.k[t][x][2 * y + 1];
+                    const uint32_t c0 = kr[t][x][2 * y], c1 = kr[t][x][2 * y + 1];
                     a[2 * x + y] = __builtin_bit_cast(bf16x8, u32x4{pair(c0, ks, lo16), pair(c0, ks, hi16), pair(c1, ks, lo16), pair(c1, ks, hi16)});
                 }
 #pragma unroll
@@ -226,6 +339,9 @@ __global__ __launch_bounds__(64 * NW) void k_cached(const __bf16 *__restrict__ Q
                 for (int x = 0; x < STEPS; ++x) s[rt][t] = mfma16(a[x], bq[rt][x], s[rt][t]);
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) load_k(p_next, jb + NW);
+        __builtin_amdgcn_sched_barrier(0);
         if (masked) {
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
@@ -235,7 +351,7 @@ __global__ __launch_bounds__(64 * NW) void k_cached(const __bf16 *__restrict__ Q
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const int key = DENSE ? 32 * (t >> 1) + 8 * kb + 4 * (t & 1) + r : 16 * kb + 4 * t + r;
-                        if (key >= left || (b.bad >> (key >> 4) & 1)) s[rt][t][r] = -INFINITY;
+                        if (key >= left || (bad >> (key >> 4) & 1)) s[rt][t][r] = -INFINITY;
                     }
             }
             // what lies behind the last key is no value at all (0 x NaN is not 0)
@@ -244,9 +360,9 @@ __global__ __launch_bounds__(64 * NW) void k_cached(const __bf16 *__restrict__ Q
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int key = 32 * st + 8 * kb + e;
-                    if (jb * KB + key >= R.keys || (b.bad >> (key >> 4) & 1))
+                    if (jb * KB + key >= R.keys || (bad >> (key >> 4) & 1))
 #pragma unroll
-                        for (int x = 0; x < VW; ++x) b.v[st][e][x] = 0u;
+                        for (int x = 0; x < VW; ++x) vr[st][e][x] = 0u;
                 }
         }
         bf16x8 p[RT][DENSE ? 2 : 1];
@@ -303,7 +419,7 @@ __global__ __launch_bounds__(64 * NW) void k_cached(const __bf16 *__restrict__ Q
             for (int st = 0; st < 2; ++st)
 #pragma unroll
                 for (int y = 0; y < 4; ++y) {
-                    const uint32_t e0 = b.v[st][2 * y][x], e1 = b.v[st][2 * y + 1][x];
+                    const uint32_t e0 = vr[st][2 * y][x], e1 = vr[st][2 * y + 1][x];
                     two[st][y][0] = __builtin_amdgcn_perm(e1, e0, 0x05010400u);
                     two[st][y][1] = __builtin_amdgcn_perm(e1, e0, 0x07030602u);
                 }
@@ -314,7 +430,7 @@ __global__ __launch_bounds__(64 * NW) void k_cached(const __bf16 *__restrict__ Q
                 for (int st = 0; st < 2; ++st)
 #pragma unroll
                     for (int y = 0; y < 4; ++y)
-                        bv[st][y] = t & 1 ? pair(two[st][y][t >> 1], b.vs[st], hi16) : pair(two[st][y][t >> 1], b.vs[st], lo16);
+                        bv[st][y] = t & 1 ? pair(two[st][y][t >> 1], v_s[st], hi16) : pair(two[st][y][t >> 1], v_s[st], lo16);
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
                     f32x4 &o = acc_o[rt][4 * x + t];
@@ -329,21 +445,13 @@ __global__ __launch_bounds__(64 * NW) void k_cached(const __bf16 *__restrict__ Q
                 }
             }
         }
-    };
-
-    {
-        Block b0, b1;
-        int jb = begin + w;
-        if (jb < end) load_block(jb, b0);
-        while (jb < end) {
-            int jn = jb + NW;
-            if (jn < end) load_block(jn, b1);
-            block(jb, b0);
-            if (jn >= end) break;
-            jb = jn + NW;
-            if (jb < end) load_block(jb, b0);
-            block(jn, b1);
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) {
+            load_v(p_next, jb + NW);
+            p_now = p_next;
+            p_next = pages(jb + 2 * NW);
         }
+        __builtin_amdgcn_sched_barrier(0);
     }
 
     // Merge: value f of lane l of wave g at float f * 64 + l of the wave's slot; a wave forms every NW-th of the four rows
@@ -377,8 +485,8 @@ __global__ __launch_bounds__(64 * NW) void k_cached(const __bf16 *__restrict__ Q
 #pragma unroll
                 for (int t = 0; t < DT; ++t) o[t] += f * from[(5 + 4 * t + r) * 64 + l];
             }
-            if constexpr (SPLIT) {
-                float *const P = part + (((long)item * RT + rt) * sz.splits + sp) * partial_floats<D>();
+            if (!alone) {
+                float *const P = part + ((long)id * RT + rt) * partial_floats<D>();
                 if (li == 0) P[row] = m, P[16 + row] = sum;
 #pragma unroll
                 for (int t = 0; t < DT; t += 4) *reinterpret_cast<f32x4 *>(P + 32 + row * D + DT * li + t) = f32x4{o[t], o[t + 1], o[t + 2], o[t + 3]};
@@ -396,29 +504,49 @@ __global__ __launch_bounds__(64 * NW) void k_cached(const __bf16 *__restrict__ Q
     }
 }
 
-// O of the row tiles whose keys several workgroups shared, in a fixed order.  One workgroup per 16 rows; a thread forms 8
-// columns of a row.  RT as in the kernel before.
+// O of the row tiles whose keys several workgroups shared (or nobody: 0), in a fixed order.  One workgroup per 16 rows; a
+// thread forms 8 columns of a row.  RT as in the kernel before.  Eight partial results are on their way at a time.
 template <int D>
 __global__ __launch_bounds__(2 * D) void k_cached_merge(const float *__restrict__ part, const int *__restrict__ cu, PagedCache cache,
                                                         Sizes sz, int RT, uint16_t *__restrict__ O) {
+    constexpr int AT_ONCE = 8;
+    const int l = threadIdx.x & 63;
+    const int x = scalar(blockIdx.x / (unsigned)RT), rt = blockIdx.x - x * RT, y = scalar(x / (unsigned)sz.tiles), tile = x - y * sz.tiles, seq = scalar(y / (unsigned)cache.Hk),
+              head = y - seq * cache.Hk;
     Rows R;
-    const int item = blockIdx.x / RT, rt = blockIdx.x - item * RT;
-    if (!R.init(sz, cu, cache, item, 16 * RT)) return;
+    if (!R.init(sz, cu, cache, seq, head, tile, 16 * RT)) return;
+    Shares sh;
+    sh.init(sz, cache, l);
+    const int nblocks = R.blocks(), shares = (nblocks + sh.per - 1) / sh.per;
+    if (shares == 1) return;
+    const int first = sh.find(sz, cache, l, 0, seq, nullptr);
     const int row = threadIdx.x / (D / 8), c = (threadIdx.x % (D / 8)) * 8, at = R.r0 + 16 * rt + row;
     if (at >= R.rows) return;
-    const int per = R.per_split(sz), shares = (R.blocks() + per - 1) / per;
-    const float *const P = part + (long)blockIdx.x * sz.splits * partial_floats<D>();
-    float m = -1.0e30f;
-    for (int sp = 0; sp < shares; ++sp) m = fmaxf(m, P[sp * partial_floats<D>() + row]);
-    float sum = 0.f;
+    const long step = (long)cache.Hk * sz.tiles * RT * partial_floats<D>();   // from a share to the next one
+    const float *P = part + (((long)first * cache.Hk + head) * sz.tiles + tile) * RT * partial_floats<D>() + rt * partial_floats<D>();
+    float m = -1.0e30f, sum = 0.f;
     f32x4 a0 = {0.f, 0.f, 0.f, 0.f}, a1 = {0.f, 0.f, 0.f, 0.f};
-    for (int sp = 0; sp < shares; ++sp) {
-        const float *const S = P + sp * partial_floats<D>();
-        const float f = __builtin_amdgcn_exp2f((S[row] - m) * sz.c);
-        const f32x4 *const src = reinterpret_cast<const f32x4 *>(S + 32 + row * D + c);
-        sum += f * S[16 + row];
-        a0 += src[0] * f;
-        a1 += src[1] * f;
+    for (int s0 = 0; s0 < shares; s0 += AT_ONCE, P += AT_ONCE * step) {
+        float ms[AT_ONCE], ls[AT_ONCE], top = m;
+        f32x4 o0[AT_ONCE], o1[AT_ONCE];
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const float *const S = P + (s0 + i < shares ? i : 0) * step;
+            const f32x4 *const src = reinterpret_cast<const f32x4 *>(S + 32 + row * D + c);
+            ms[i] = S[row], ls[i] = S[16 + row], o0[i] = src[0], o1[i] = src[1];
+        }
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) top = fmaxf(top, ms[i]);
+        const float f = __builtin_amdgcn_exp2f((m - top) * sz.c);
+        m = top;
+        sum *= f, a0 *= f, a1 *= f;
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const float g = s0 + i < shares ? __builtin_amdgcn_exp2f((ms[i] - m) * sz.c) : 0.f;
+            sum += g * ls[i];
+            a0 += o0[i] * g;
+            a1 += o1[i] * g;
+        }
     }
     const float inv = sum > 0.f ? 1.f / sum : 0.f;
     a0 *= inv, a1 *= inv;
@@ -427,48 +555,48 @@ __global__ __launch_bounds__(2 * D) void k_cached_merge(const float *__restrict_
         pack_bf16x2(a0[0], a0[1]), pack_bf16x2(a0[2], a0[3]), pack_bf16x2(a1[0], a1[1]), pack_bf16x2(a1[2], a1[3])};
 }
 
-constexpr int waves_of(int d) { return d == 64 ? 8 : 4; }
 // 16-row tiles of a workgroup
 int row_tiles(long rows) { return rows <= 16 ? 1 : 2; }
 
 struct Plan {
-    int RT, tiles, splits, least;
+    int RT, NW, tiles, target, least;   // NW: waves of a workgroup; target 0: nobody shares
 };
 Plan plan(int B, int Hk, int G, int most, int max_len, int d) {
     Plan p;
     const long rows = (long)most * G;
     p.RT = row_tiles(rows);
     p.tiles = (int)((rows + 16 * p.RT - 1) / (16 * p.RT));
-    const long items = (long)B * Hk * p.tiles;
-    const int blocks = (max_len + KB - 1) / KB, nw = waves_of(d);
-    p.least = nw;                                 // at least a block for each wave
-    long n = 512 / items;                         // two workgroups to a compute unit
-    const long by_length = blocks / 64;           // and none of more than 4096 keys: sequences differ in length
-    n = n > by_length ? n : by_length;
-    const long most_splits = (blocks + p.least - 1) / p.least;
-    n = n < most_splits ? n : most_splits;
-    n = n < (1 << 22) / items ? n : (1 << 22) / items;   // (a launch has fewer than 2^32 threads)
-    p.splits = n < 1 ? 1 : (int)n;
+    const long per_share = (long)Hk * p.tiles, items = B * per_share;   // workgroups of a share, and without shares
+    const int blocks = (max_len + KB - 1) / KB;
+    p.NW = items <= 256 ? 8 : 4;
+    p.target = 0;
+    if (blocks <= 5 * p.NW || (long)B * blocks > 1 << 30) return p;
+    if (items * blocks <= 4096) p.NW = 4;
+    const long slots = p.NW == 8 ? 256 : 512;
+    if (items >= 4 * slots || (items >= slots && blocks < 128)) return p;
+    p.least = p.NW;
+    const long fit = slots / per_share - B;       // (the last share of a sequence is cut short)
+    long t = fit > B / 2 ? fit : B / 2 > 0 ? B / 2 : 1;
+    const long most_shares = (long)B * ((blocks + p.least - 1) / p.least);
+    p.target = (int)(t < most_shares ? t : most_shares);
     return p;
 }
+// Shares of all sequences, at most (of a valid plan that shares)
+long shares_of(const Plan &p, int B) { return (long)p.target + B; }
 
-template <int D, int MODE, int RT>
+template <int D, int MODE, int RT, int NW>
 hipError_t launch(const HeadRows &Q, int T, const int *cu, int B, int most, int max_len, float scale, bool causal,
                   const PagedCache &c, void *O, float *part, const Plan &p, hipStream_t st) {
-    constexpr int NW = waves_of(D);
-    const Sizes sz = {T, B, Q.H, Q.H / c.Hk, most, max_len, p.tiles, p.splits, p.least, Q.token, Q.head,
+    const Sizes sz = {T, B, Q.H, Q.H / c.Hk, most, max_len, p.tiles, p.target, p.least, Q.token, Q.head, p.target ? 1. / p.target : 0.,
                       scale * 1.4426950408889634f, causal ? 1 : 0};
-    const unsigned items = (unsigned)((long)B * c.Hk * p.tiles);
-#define DFSS_LAUNCH(SPLIT)                                                                                              \
-    hipLaunchKernelGGL((k_cached<D, MODE, NW, RT, SPLIT>), dim3(items * p.splits), dim3(64 * NW), 0, st,               \
+    const unsigned items = (unsigned)((long)B * c.Hk * p.tiles), shares = (unsigned)(shares_of(p, B) * c.Hk * p.tiles);
+#define DFSS_LAUNCH(BIG)                                                                                                \
+    hipLaunchKernelGGL((k_cached<D, MODE, NW, RT, BIG>), dim3(p.target ? shares : items), dim3(64 * NW), 0, st,         \
                        (const __bf16 *)Q.data, cu, c, c.k, c.v, c.k_scale, c.v_scale, c.table, sz, (uint16_t *)O, part)
-    if (p.splits > 1) {
-        DFSS_LAUNCH(true);
-        hipLaunchKernelGGL(k_cached_merge<D>, dim3(items * RT), dim3(2 * D), 0, st, part, cu, c, sz, RT, (uint16_t *)O);
-    } else {
-        DFSS_LAUNCH(false);
-    }
+    if (c.page_shift >= 6) DFSS_LAUNCH(true); else DFSS_LAUNCH(false);
 #undef DFSS_LAUNCH
+    if (p.target)
+        hipLaunchKernelGGL(k_cached_merge<D>, dim3(items * RT), dim3(2 * D), 0, st, part, cu, c, sz, RT, (uint16_t *)O);
     return hipGetLastError();
 }
 
@@ -476,17 +604,19 @@ hipError_t launch(const HeadRows &Q, int T, const int *cu, int B, int most, int 
 
 size_t cached_workspace_bytes(int B, int Hq, int Hk, int most, int max_len, int d) {
     const Plan p = plan(B, Hk, Hq / Hk, most, max_len, d);
-    return p.splits == 1 ? 0 : (size_t)B * Hk * p.tiles * p.RT * p.splits * 16 * (d + 2) * sizeof(float);
+    return p.target ? (size_t)shares_of(p, B) * Hk * p.tiles * p.RT * 16 * (d + 2) * sizeof(float) : 0;
 }
 
 hipError_t launch_attention_cached(const HeadRows &Q, int T, const int *cu, int B, int most, int max_len, int d, int mode,
                                    float scale, bool causal, const PagedCache &c, void *O, void *part, hipStream_t st) {
     const Plan p = plan(B, c.Hk, Q.H / c.Hk, most, max_len, d);
-#define DFSS_CALL(D, M, RT) launch<D, M, RT>(Q, T, cu, B, most, max_len, scale, causal, c, O, (float *)part, p, st)
-#define DFSS_MODE(D, M) (p.RT == 1 ? DFSS_CALL(D, M, 1) : DFSS_CALL(D, M, 2))
+#define DFSS_CALL(D, M, RT, NW) launch<D, M, RT, NW>(Q, T, cu, B, most, max_len, scale, causal, c, O, (float *)part, p, st)
+#define DFSS_WAVES(D, M, RT) (p.NW == 8 ? DFSS_CALL(D, M, RT, 8) : DFSS_CALL(D, M, RT, 4))
+#define DFSS_MODE(D, M) (p.RT == 1 ? DFSS_WAVES(D, M, 1) : DFSS_WAVES(D, M, 2))
     if (d == 64) return mode == 0 ? DFSS_MODE(64, MODE_2TO4) : mode == 1 ? DFSS_MODE(64, MODE_1TO2) : DFSS_MODE(64, MODE_DENSE);
     return mode == 0 ? DFSS_MODE(128, MODE_2TO4) : mode == 1 ? DFSS_MODE(128, MODE_1TO2) : DFSS_MODE(128, MODE_DENSE);
 #undef DFSS_MODE
+#undef DFSS_WAVES
 #undef DFSS_CALL
 }
 

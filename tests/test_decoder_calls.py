@@ -8,7 +8,7 @@ import torch
 
 import paper_2203_00091_amd as dfss
 from paper_2203_00091_amd import Shape
-from paper_2203_00091_amd.binding import _CCache, _CRotary, _CRows
+from paper_2203_00091_amd import binding
 
 OK, NULL, SHAPE, UNSUP, WS = 0, 1, 2, 3, 4
 
@@ -22,19 +22,15 @@ class Host:
         self.lib = dfss.load_library()
 
     def rows(self, H=4, batch=0, token=256, head=64, data=None):
-        return _CRows(self.a if data is None else data, H, batch, token, head)
+        return binding._ROWS.pack(self.a if data is None else data, H, batch, token, head)
 
     def rotary(self, **kw):
-        r = _CRotary(self.a, self.a, None, 10, 64, 0)
-        for k, v in kw.items():
-            setattr(r, k, v)
-        return r
+        r = dict(cos=self.a, sin=self.a, pos=0, n_pos=10, rot=64, interleaved=0) | {k: v or 0 for k, v in kw.items()}
+        return binding._ROTARY.pack(*r.values())
 
     def cache(self, **kw):
-        c = _CCache(self.a, self.a, self.a, self.a, self.a, self.a, 8, 2, 64, 4)
-        for k, v in kw.items():
-            setattr(c, k, v)
-        return c
+        c = {k: self.a for k in ("k", "v", "k_scale", "v_scale", "table", "len")} | dict(n_pages=8, Hk=2, page=64, width=4)
+        return binding._CACHE.pack(*(c | {k: v or 0 for k, v in kw.items()}).values())
 
 
 @pytest.fixture

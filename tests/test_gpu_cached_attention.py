@@ -268,7 +268,7 @@ def test_long_sequences_are_shared(d, mode):
     got = [a.call(*mode, ws=torch.full((need,), fill, dtype=torch.uint8, device=DEV)) for fill in (0, 255)]
     assert torch.equal(got[0], got[1]) and torch.equal(got[0], a.call(*mode))
     a.check(got[0], *mode)
-    b = Attend(d, 16, 1, 3, [(2500, 40), (1100, 7)], 36)
+    b = Attend(d, 16, 1, 3, [(2700, 40), (1100, 7)], 36)
     assert dfss.dfss_cached_workspace_bytes(b.shape(*mode), b.cache) > 0
     b.check(b.call(*mode), *mode)
 

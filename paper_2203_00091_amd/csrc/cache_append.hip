@@ -6,10 +6,11 @@
 // operands from one conversion instruction, exactly, and because codes that a larger scale replaces keep their three bits
 // of fraction (only those that become subnormal are rounded again).
 //
-// Bound by memory (2 bytes read and 1 written for each value), and by latency where a sequence gets one token.  A
-// workgroup owns what a call adds to one page of one head, of K or of V, so that nobody else touches the page's scale:
-// it holds the new rows in registers, finds their amax, and with the old scale, where the page holds earlier tokens, the
-// new one; the earlier codes are read and written only if it grew.
+// Bound by memory (2 bytes read and 1 written for each value), and by latency where a sequence gets one token.  What a call
+// adds to one page of one head, of K or of V, is a unit's, so that nobody else touches the page's scale: it holds the new rows
+// in registers, finds their amax, and with the old scale, where the page holds earlier tokens, the new one; the earlier codes are
+// read and written only if it grew.  A unit is a wave where eight of its passes (8 elements in each lane) hold the rows, else a
+// workgroup.
 #include "dfss_kernels.hpp"
 #include "head_rows.hpp"
 
@@ -43,44 +44,52 @@ __device__ __forceinline__ void decode(u32x2 c, float *x) {
     }
 }
 
-// Grid: x = slots, y = head, z = 0 for K and 1 for V.  Sequence b has the slots from cu[b] / page + 2 b on: more than the
-// pages that its tokens lie in ((n - 1) / page + 2 at most), and sequence and page follow from the slot by one look at cu.
-// NP passes of 2048 / D rows make up a page.
-template <int D, int NP>
+// Grid: x = slots, y = K and V of the heads: a unit takes `each` of them, one after the other.  Sequence b has the slots from cu[b] / page + 2 b
+// on: more than the pages that its tokens lie in ((n - 1) / page + 2 at most), and sequence and page follow from the slot by one look
+// at cu.
+template <int D, int WU, int NP>
 __global__ __launch_bounds__(256) void k_cache_append(HeadRows K, HeadRows V, int T, const int *__restrict__ cu, int B, int most,
                                                       int max_len, const __bf16 *__restrict__ w, float eps, RotaryTable rt,
-                                                      PagedCache cache) {
-    constexpr int LPR = D / 8, RPP = 256 / LPR;
+                                                      PagedCache cache, int each) {
+    constexpr int LPR = D / 8, RPP = 64 * WU / LPR;   // lanes of a row; rows of a pass
     __shared__ float amax4[4];
-    const int l = threadIdx.x & 63, c = threadIdx.x % LPR, row = threadIdx.x / LPR;
-    const int page = 1 << cache.page_shift, head = blockIdx.y;
-    const bool is_v = blockIdx.z != 0;
+    const int l = threadIdx.x & 63, c = threadIdx.x % LPR, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int row = (WU == 1 ? l : (int)threadIdx.x) / LPR;
+    const int page = 1 << cache.page_shift;
+    // (the four waves of a workgroup take neighbouring heads, whose rows are one piece of the token's)
+    constexpr int STEP = WU == 1 ? 4 : 1;
+    const bool is_v = blockIdx.y & 1;
+    const int group = ((int)blockIdx.y >> 1) * each * STEP, head0 = group + (WU == 1 ? wave : 0);
+    const int heads = group + each * STEP < cache.Hk ? group + each * STEP : cache.Hk;
+    if (head0 >= heads) return;
 
-    int b, lo, n, slot;
+    int b = -1, lo = 0, n = 0, slot = 0, len = 0;
     if (cu) {
-        int before = 0;   // sequences whose slots begin at or before this one
-        for (int i = 0; i < B; i += 64) {
-            const int at = i + l < B ? i + l : B - 1;
-            int first = cu[at];
-            first = first < 0 ? 0 : first < T ? first : T;
-            before += __popcll(__ballot(i + l < B && (first >> cache.page_shift) + 2 * at <= (int)blockIdx.x));
+        for (int i = 0; i < B; i += 64) {   // 64 sequences at a time: the last whose slots begin at or before this one
+            const int at = i + l < B ? i + l : B - 1, length = cache.len[at];
+            int from = cu[at], to = cu[at + 1];
+            from = from < 0 ? 0 : from < T ? from : T;
+            to = to < from ? from : to < T ? to : T;
+            const int first = (from >> cache.page_shift) + 2 * at;
+            const uint64_t before = __ballot(i + l < B && first <= (int)blockIdx.x);
+            if (!before) break;
+            const int lane = 63 - __builtin_clzll(before);
+            b = i + lane;
+            lo = __builtin_amdgcn_readlane(from, lane);
+            n = __builtin_amdgcn_readlane(to, lane) - lo;
+            slot = (int)blockIdx.x - __builtin_amdgcn_readlane(first, lane);
+            len = __builtin_amdgcn_readlane(length, lane);
         }
-        if (before == 0) return;
-        b = before - 1;
-        lo = cu[b], n = cu[b + 1];
-        lo = lo < 0 ? 0 : lo < T ? lo : T;
-        n = n < lo ? lo : n < T ? n : T;
-        n -= lo;
-        slot = (int)blockIdx.x - (lo >> cache.page_shift) - 2 * b;
     } else {
         const int per = (most - 1) / page + 2;
-        b = (int)blockIdx.x / per;
+        b = __builtin_amdgcn_readfirstlane((int)blockIdx.x / per);
         slot = (int)blockIdx.x - b * per;
         lo = b * most;
         n = most;
+        len = cache.len[b];
     }
     if (n <= 0) return;
-    const int len = cache.len[b] < 0 ? 0 : cache.len[b];
+    len = len < 0 ? 0 : len;
     const long capacity = (long)cache.width << cache.page_shift;
     const int limit = max_len < capacity ? max_len : (int)capacity;   // tokens from here on are not kept
     const int start = len - n;
@@ -90,101 +99,152 @@ __global__ __launch_bounds__(256) void k_cache_append(HeadRows K, HeadRows V, in
     if (p >= cache.width || first >= end) return;
     const int id = cache.table[(long)b * cache.width + p];
     if ((unsigned)id >= (unsigned)cache.n_pages) return;   // no such page: its tokens are not kept
-    const int s0 = first - p * page, s1 = end - p * page;  // the page's rows that are written
+    const int s0 = first - p * page, rows = end - first;   // the page's rows that are written
     const HeadRows &X = is_v ? V : K;
-    const __bf16 *const src = static_cast<const __bf16 *>(X.data) + head * X.head + 8 * c;
-    const long token0 = (long)lo + (p * (long)page - start);   // the token of the page's row 0 (may lie before the first)
+    const long token0 = (long)lo + (first - start);         // token of row s0
+    const __bf16 *const src = static_cast<const __bf16 *>(X.data) + token0 * X.token + 8 * c;
 
-    Eight<__bf16> raw[NP];
+    Eight<__bf16> w_mine, w_other, raw[NP];
+    if (w) w_mine.load(w + 8 * c);
+    float x[NP][8], old = 0.f;
+    float *const scales = static_cast<float *>(is_v ? cache.v_scale : cache.k_scale) + (long)id * cache.Hk;
+    auto load = [&](int head, int g0) {
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        const int r = i * RPP + row;
-        raw[i].clear();
-        if (r >= s0 && r < s1) raw[i].load(src + (token0 + r) * X.token);
-    }
-    float x[NP][8], amax = 0.f;
+        for (int i = 0; i < NP; ++i) {
+            const int r = g0 + i * RPP + row;
+            raw[i].clear();
+            if (r < rows) raw[i].load(src + r * X.token + head * X.head);
+        }
+    };
+    // x = the values of the new rows g0 .. g0 + NP RPP - 1 (0 where there are fewer), from raw
+    auto values = [&](int g0) {
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        const int r = i * RPP + row;
-        raw[i].get(x[i]);
-        if (!is_v && (i * RPP < s1 && (i + 1) * RPP > s0)) {   // (the same in every lane)
+        for (int i = 0; i < NP; ++i) {
+            raw[i].get(x[i]);
+            if (is_v || g0 + i * RPP >= rows) continue;
+            const int r = g0 + i * RPP + row;
             const long token = token0 + r;
-            const bool real = r >= s0 && r < s1;
             Turn turn;
-            turn.load(rt.cos, rt.sin, real ? rt.at(token, start + (token - lo)) : 0, rt.rot, rt.interleaved != 0, l, c, false);
+            turn.load(rt.cos, rt.sin, r < rows ? rt.at(token, start + (token - lo)) : 0, rt.rot, rt.interleaved != 0, l, c, false);
             float xo[8];
             raw[i].of_lane(turn.other).get(xo);
-            // In 64 bits: a code has a border every 16th of its value, and each 32-bit rounding on the way would put a few of a
-            // million values on the wrong side of theirs.  (Free here: 24 operations for three bytes that pass the memory.)
-            double f[8], fo[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = x[i][e], fo[e] = xo[e];
+            // y = r (x w cos + x' w' sin) in 64 bits (x w is exact in 32): a code has a border every 16th of its value, and each 32-bit
+            // rounding on the way would put a few of a million values on the wrong side of theirs.
+            double rn = 1.;
             if (w) {
                 double ss = 0.;
-                float wf[8];
+                float f[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) ss += f[e] * f[e];
+                for (int e = 0; e < 8; ++e) ss += (double)(x[i][e] * x[i][e]);
 #pragma unroll
                 for (int o = LPR / 2; o > 0; o >>= 1) ss += __shfl_xor(ss, o, kWave);
-                const double rn = 1. / __builtin_sqrt(ss * (1. / D) + eps);
-                Eight<__bf16> v;
-                v.load(w + 8 * c);
-                v.get(wf);
+                ss = ss * (1. / D) + eps;
+                rn = __builtin_amdgcn_rsqf((float)ss);   // 1 / sqrt in 32 bits, and a step of Newton's for 40 and more
+                rn = rn * (1.5 - 0.5 * ss * rn * rn);
+                w_mine.get(f);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] *= rn * wf[e];
-                v.load(w + 8 * (turn.other % LPR));
-                v.get(wf);
+                for (int e = 0; e < 8; ++e) x[i][e] *= f[e];
+                if (i == 0) w_other.load(w + 8 * (turn.other % LPR));   // (the same chunk in every pass)
+                w_other.get(f);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) fo[e] *= rn * wf[e];
+                for (int e = 0; e < 8; ++e) xo[e] *= f[e];
             }
+            float y[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[i][e] = (float)(f[e] * turn.cos[e] + (turn.interleaved ? f[e ^ 1] : fo[e]) * turn.sin[e]);
+            for (int e = 0; e < 8; ++e)
+                y[e] = (float)(rn * __builtin_fma((double)x[i][e], (double)turn.cos[e], (double)(turn.interleaved ? x[i][e ^ 1] : xo[e]) * (double)turn.sin[e]));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[i][e] = y[e];
+        }
+    };
+    // Rows that the registers hold.  Of more of them (launch_cache_append: only with NP = 1) the values are formed twice.
+    constexpr int GROUP = NP * RPP;
+    const bool held = NP > 1 || rows <= GROUP;
+    load(head0, 0);
+    if (s0 > 0) old = scales[head0];
+    for (int head = head0; head < heads; head += STEP) {
+        uint8_t *const codes = (is_v ? cache.v : cache.k) + (((long)id * cache.Hk + head) << cache.page_shift) * D + 8 * c;
+        auto store = [&](int g0, float inv) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const int r = g0 + i * RPP + row;
+                if (r < rows) *reinterpret_cast<u32x2 *>(codes + (long)(s0 + r) * D) = encode(x[i], inv);
+            }
+        };
+        float amax = 0.f;
+        const float before = old;
+        for (int g0 = 0; g0 < (held ? 1 : rows); g0 += GROUP) {
+            if (g0 > 0) load(head, g0);
+            values(g0);
+#pragma unroll
+            for (int i = 0; i < NP; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) amax = fmaxf(amax, __builtin_fabsf(x[i][e]));
+        }
+        if (held && head + STEP < heads) {   // the next head's are on their way
+            load(head + STEP, 0);
+            if (s0 > 0) old = scales[head + STEP];
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) amax = fmaxf(amax, __builtin_fabsf(x[i][e]));
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o, kWave));
-    if (l == 0) amax4[threadIdx.x >> 6] = amax;
-    float *const scale = (is_v ? cache.v_scale : cache.k_scale) + (long)id * cache.Hk + head;
-    uint8_t *const codes = (is_v ? cache.v : cache.k) + (((long)id * cache.Hk + head) << cache.page_shift) * D + 8 * c;
-    const float old = s0 > 0 ? *scale : 0.f;
-    __syncthreads();   // (also: everybody has read the old scale)
-    const int e = scale_exponent(fmaxf(fmaxf(amax4[0], amax4[1]), fmaxf(amax4[2], amax4[3])));
-    float now = exp2_int(e);
-    if (old >= now) {
-        now = old;
-    } else if (s0 > 0) {
-        const float ratio = old / now;   // (both powers of two)
-        for (int r = row; r < s0; r += RPP) {
-            u32x2 *const at = reinterpret_cast<u32x2 *>(codes + (long)r * D);
-            float v[8];
-            decode(*at, v);
-            *at = encode(v, ratio);
+        for (int o = 32; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o, kWave));
+        if constexpr (WU == 4) {
+            __syncthreads();   // (the last head's have been read)
+            if (l == 0) amax4[wave] = amax;
+            __syncthreads();   // (also: everybody has read the old scale)
+            amax = fmaxf(fmaxf(amax4[0], amax4[1]), fmaxf(amax4[2], amax4[3]));
         }
-    }
-    if (threadIdx.x == 0) *scale = now;
-    const float inv = 1.f / now;
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        const int r = i * RPP + row;
-        if (r >= s0 && r < s1) *reinterpret_cast<u32x2 *>(codes + (long)r * D) = encode(x[i], inv);
+        float now = exp2_int(scale_exponent(amax));
+        if (before >= now) {
+            now = before;
+        } else if (s0 > 0) {
+            const float ratio = before / now;   // (both powers of two)
+            for (int r = row; r < s0; r += RPP) {
+                u32x2 *const at = reinterpret_cast<u32x2 *>(codes + (long)r * D);
+                float v[8];
+                decode(*at, v);
+                *at = encode(v, ratio);
+            }
+        }
+        if ((WU == 1 ? l : (int)threadIdx.x) == 0) scales[head] = now;
+        const float inv = 1.f / now;
+        if (held) {
+            store(0, inv);
+            continue;
+        }
+        for (int g0 = 0; g0 < rows; g0 += GROUP) {
+            load(head, g0);
+            values(g0);
+            store(g0, inv);
+        }
+        if (head + STEP < heads) {
+            load(head + STEP, 0);
+            if (s0 > 0) old = scales[head + STEP];
+        }
     }
 }
+
+constexpr long kFullWaves = 4096;
 
 }  // namespace
 
 hipError_t launch_cache_append(const HeadRows &K, const HeadRows &V, int T, const int *cu, int B, int most, int max_len, int d,
                                const void *w, float eps, const RotaryTable &rt, const PagedCache &c, hipStream_t st) {
-    const int page = 1 << c.page_shift, passes = page * d / 2048;
+    const int page = 1 << c.page_shift;
     const unsigned slots = cu ? (unsigned)(T / page + 2 * B) : (unsigned)B * (unsigned)((most - 1) / page + 2);
-    const dim3 grid(slots, (unsigned)c.Hk, 2);
-#define DFSS_LAUNCH(D, NP)                                                                                              \
-    hipLaunchKernelGGL((k_cache_append<D, NP>), grid, dim3(256), 0, st, K, V, T, cu, B, most, max_len, (const __bf16 *)w, eps, rt, c)
+    // Rows that a call adds to a page, at most -- or, where the calls are those of a step of generation (about a token for each
+    // sequence), most likely.  As few registers as those rows need: of many short units waves wait for memory one after the other.
+    const int added = cu ? (T <= 2 * B ? 2 : T) : most, rows = page < added ? page : added, passes = (rows * (d / 8) + 63) / 64;
+    const bool wave = passes <= 8;
+    // heads that a unit takes one after the other, its next rows on their way: as many as leave the chip full
+    const long waves = (long)slots * 2 * c.Hk * (wave ? 1 : 4);
+    const int each = waves >= 4 * kFullWaves ? 4 : waves >= 2 * kFullWaves ? 2 : 1, heads = each * (wave ? 4 : 1);
+    const dim3 grid(slots, 2 * (unsigned)((c.Hk + heads - 1) / heads));
+#define DFSS_LAUNCH(D, WU, NP)                                                                                          \
+    hipLaunchKernelGGL((k_cache_append<D, WU, NP>), grid, dim3(256), 0, st, K, V, T, cu, B, most, max_len, (const __bf16 *)w, eps, rt, c, each)
     if (d == 64) {
-        if (passes <= 1) DFSS_LAUNCH(64, 1); else if (passes == 2) DFSS_LAUNCH(64, 2); else DFSS_LAUNCH(64, 4);
+        if (passes <= 1) DFSS_LAUNCH(64, 1, 1); else if (passes <= 2) DFSS_LAUNCH(64, 1, 2); else if (passes <= 4) DFSS_LAUNCH(64, 1, 4); else if (wave) DFSS_LAUNCH(64, 1, 8); else DFSS_LAUNCH(64, 4, 4);
     } else {
-        if (passes <= 1) DFSS_LAUNCH(128, 1); else if (passes == 2) DFSS_LAUNCH(128, 2); else if (passes == 4) DFSS_LAUNCH(128, 4); else DFSS_LAUNCH(128, 8);
+        if (passes <= 1) DFSS_LAUNCH(128, 1, 1); else if (passes <= 2) DFSS_LAUNCH(128, 1, 2); else if (passes <= 4) DFSS_LAUNCH(128, 1, 4); else if (wave) DFSS_LAUNCH(128, 1, 8); else DFSS_LAUNCH(128, 4, 8);
     }
 #undef DFSS_LAUNCH
     return hipGetLastError();

@@ -7,8 +7,9 @@
 // All of it in 32 bits, rounded once at the end.
 //
 // Bound by memory: every element is read and written once (the backward pass reads x and dy).  A lane holds eight
-// elements of a row, so a row is d / 8 lanes; a wave takes one token and HPW x U heads of it, so that the angles are read
-// once for all of them, and all its loads are on their way before the first is used.
+// elements of a row, so a row is d / 8 lanes; the rows that a wave holds side by side are one head's of consecutive tokens (what it
+// writes to the attention's layout is 1 KiB in a piece), and it goes through heads, U of them on their way at a time: the angles
+// are read once for all of them.
 #include "dfss_kernels.hpp"
 #include "head_rows.hpp"
 
@@ -16,140 +17,160 @@ namespace dfss {
 
 namespace {
 
-// Row of head h, counted through those of Q and then of K.
-template <typename T>
-__device__ __forceinline__ T *row(const HeadRows &Q, const HeadRows &K, int h, long b, long t) {
-    const bool q = h < Q.H;
-    return static_cast<T *>(q ? Q.data : K.data) + b * (q ? Q.batch : K.batch) + t * (q ? Q.token : K.token) +
-           (q ? h : h - Q.H) * (q ? Q.head : K.head);
-}
+// A lane's place: its token (a batch element's, or none behind the last one) and its eight elements of a row.
+struct Place {
+    long token, b, t;
+    int c, lane;
+    bool real;
+    template <int LPR>
+    static __device__ __forceinline__ Place of(long first, long tokens, int L) {
+        Place p;
+        p.lane = threadIdx.x & 63, p.c = p.lane % LPR;
+        const long i = first + p.lane / LPR;
+        p.real = i < tokens;
+        p.token = p.real ? i : tokens - 1;
+        p.b = tokens <= 0x7FFFFFFF ? (long)((unsigned)p.token / (unsigned)L) : p.token / L;
+        p.t = p.token - p.b * L;
+        return p;
+    }
+    template <typename T>
+    __device__ __forceinline__ T *row(const HeadRows &R, int h) const {
+        return static_cast<T *>(R.data) + b * R.batch + t * R.token + h * R.head + 8 * c;
+    }
+};
 
+// Eight weights of a lane, and those of the elements that turn with them.
+template <typename T>
+struct Weights {
+    Eight<T> mine, other;
+    __device__ __forceinline__ void load(const T *w, const Place &p, const Turn &turn, int LPR) {
+        mine.load(w + 8 * p.c);
+        other.load(w + 8 * (turn.other % LPR));
+    }
+};
+
+// A wave: 64 / (d / 8) tokens, and `each` of the heads of Q and then of K.
 template <typename T, int D, int U>
 __global__ __launch_bounds__(256) void k_norm_rotate(HeadRows Q, HeadRows K, const T *__restrict__ wq, const T *__restrict__ wk,
-                                                     float eps, RotaryTable rt, long tokens, int L, HeadRows Qo, HeadRows Ko) {
-    constexpr int LPR = D / 8, HPW = 64 / LPR;
-    const int l = threadIdx.x & 63, c = l % LPR, g = l / LPR;
-    const int heads = Q.H + K.H, parts = (heads + HPW * U - 1) / (HPW * U);
-    const long unit = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const long token = unit / parts;
-    if (token >= tokens) return;
-    const int h0 = (int)(unit - token * parts) * HPW * U + g;
-    const long b = token / L, t = token - b * L;
-
-    Eight<T> x[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int h = h0 + u * HPW;
-        x[u].clear();
-        if (h < heads) {
-            x[u].load(row<T>(Q, K, h, b, t) + 8 * c);
-        }
-    }
+                                                     float eps, RotaryTable rt, long tokens, int L, HeadRows Qo, HeadRows Ko,
+                                                     int parts, int each) {
+    constexpr int LPR = D / 8, TPW = 64 / LPR;
+    const unsigned unit = blockIdx.x * 4 + (unsigned)__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const unsigned group = __builtin_amdgcn_readfirstlane(unit / (unsigned)parts);
+    if ((long)group * TPW >= tokens) return;
+    const int from = (int)(unit - group * parts) * each, heads = Q.H + K.H, to = from + each < heads ? from + each : heads;
+    const Place at = Place::of<LPR>((long)group * TPW, tokens, L);
     Turn turn;
-    turn.load(rt.cos, rt.sin, rt.at(token, t), rt.rot, rt.interleaved != 0, l, c, false);
+    turn.load(rt.cos, rt.sin, rt.at(at.token, at.t), rt.rot, rt.interleaved != 0, at.lane, at.c, false);
+    // the part's heads of Q, then those of K
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int h = h0 + u * HPW;
-        const T *const w = h < Q.H ? wq : wk;
-        float a[8], ao[8], y[8], r = 1.f;
-        x[u].get(a);
-        x[u].of_lane(turn.other).get(ao);
-        if (wq || wk) {
-            float ss = 0.f;
+    for (int side = 0; side < 2; ++side) {
+        const HeadRows &X = side ? K : Q, &Y = side ? Ko : Qo;
+        const int first = side ? (from > Q.H ? from - Q.H : 0) : from, last = side ? to - Q.H : (to < Q.H ? to : Q.H);
+        const T *const w = side ? wk : wq;
+        Weights<T> ws;
+        if (w && first < last) ws.load(w, at, turn, LPR);
+        for (int h = first; h < last; h += U) {
+            Eight<T> x[U];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) ss = __builtin_fmaf(a[e], a[e], ss);
-            ss = row_sum<LPR>(ss);
-            if (w) {
-                r = 1.f / __builtin_sqrtf(ss * (1.f / D) + eps);
-                Eight<T> v;
-                float f[8];
-                v.load(w + 8 * c);
-                v.get(f);
+            for (int u = 0; u < U; ++u)
+                if (h + u < last) x[u].load(at.row<T>(X, h + u));
 #pragma unroll
-                for (int e = 0; e < 8; ++e) a[e] *= r * f[e];
-                v.load(w + 8 * (turn.other % LPR));
-                v.get(f);
+            for (int u = 0; u < U; ++u) {
+                if (h + u >= last) break;
+                float a[8], ao[8], y[8];
+                x[u].get(a);
+                x[u].of_lane(turn.other).get(ao);
+                if (w) {
+                    float ss = 0.f, f[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) ao[e] *= r * f[e];
+                    for (int e = 0; e < 8; ++e) ss = __builtin_fmaf(a[e], a[e], ss);
+                    const float r = 1.f / __builtin_sqrtf(row_sum<LPR>(ss) * (1.f / D) + eps);
+                    ws.mine.get(f);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) a[e] *= r * f[e];
+                    ws.other.get(f);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) ao[e] *= r * f[e];
+                }
+                turn.apply(a, ao, y);
+                x[u].set(y);
+                if (at.real) x[u].store(at.row<T>(Y, h + u));
             }
-        }
-        turn.apply(a, ao, y);
-        if (h < heads) {
-            x[u].set(y);
-            x[u].store(row<T>(Qo, Ko, h, b, t) + 8 * c);
         }
     }
 }
 
 // Workgroups of the backward pass, queries and keys together: each leaves one partial sum of dw.
-constexpr int kGradGroups = 512;
+constexpr int kGradGroups = 1024;
+constexpr long kForwardWaves = 8192;
 
-// Queries in the first `qgroups` workgroups, keys in the others; a wave goes over units of one token and HPW x U heads.
+__device__ __forceinline__ HeadRows either(bool first, const HeadRows &a, const HeadRows &b) {
+    return HeadRows{first ? a.data : b.data, first ? a.batch : b.batch, first ? a.token : b.token, first ? a.head : b.head, first ? a.H : b.H};
+}
+
+// Queries in the first `qgroups` workgroups, keys in the others; a wave goes over units of 64 / (d / 8) tokens and `each` heads.
 template <typename T, int D, int U>
-__global__ __launch_bounds__(256) void k_norm_rotate_grad(HeadRows dQo, HeadRows dKo, HeadRows Q, HeadRows K,
+__global__ __launch_bounds__(256, 4) void k_norm_rotate_grad(HeadRows dQo, HeadRows dKo, HeadRows Q, HeadRows K,
                                                           const T *__restrict__ wq, const T *__restrict__ wk, float eps,
                                                           RotaryTable rt, long tokens, int L, HeadRows dQ, HeadRows dK,
-                                                          int qgroups, float *__restrict__ part) {
-    constexpr int LPR = D / 8, HPW = 64 / LPR;
+                                                          int qgroups, int each, float *__restrict__ part) {
+    constexpr int LPR = D / 8, TPW = 64 / LPR;
     __shared__ float sums[4][D];
-    const int l = threadIdx.x & 63, c = l % LPR, g = l / LPR, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = threadIdx.x & 63;
     const bool key = (int)blockIdx.x >= qgroups;
-    const HeadRows &Y = key ? dKo : dQo, &X = key ? K : Q, &dX = key ? dK : dQ;
+    const HeadRows Y = either(key, dKo, dQo), X = either(key, K, Q), dX = either(key, dK, dQ);
     const T *const w = key ? wk : wq;
     const int group = key ? blockIdx.x - qgroups : blockIdx.x, groups = key ? gridDim.x - qgroups : qgroups;
-    const int parts = (X.H + HPW * U - 1) / (HPW * U);
-    const long units = tokens * parts;
-    float f[8], dw[8];
+    // (whatever follows from a division is vector work unless it is read back)
+    const int parts = __builtin_amdgcn_readfirstlane((X.H + each - 1) / each);
+    const long units = (tokens + TPW - 1) / TPW * parts;
+    float dw[8];
+    Eight<T> wv;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = 1.f, dw[e] = 0.f;
-    if (w) {
-        Eight<T> v;
-        v.load(w + 8 * c);
-        v.get(f);
-    }
+    for (int e = 0; e < 8; ++e) dw[e] = 0.f;
+    if (w) wv.load(w + 8 * (l % LPR));
     for (long unit = (long)group * 4 + wave; unit < units; unit += 4L * groups) {
-        const long token = unit / parts, b = token / L, t = token - b * L;
-        const int h0 = (int)(unit - token * parts) * HPW * U + g;
-        Eight<T> y[U], x[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int h = h0 + u * HPW;
-            y[u].clear();
-            x[u].clear();
-            if (h < X.H) {
-                y[u].load(static_cast<const T *>(Y.data) + b * Y.batch + t * Y.token + h * Y.head + 8 * c);
-                if (w) x[u].load(static_cast<const T *>(X.data) + b * X.batch + t * X.token + h * X.head + 8 * c);
-            }
-        }
+        const unsigned tg = __builtin_amdgcn_readfirstlane((unsigned)unit / (unsigned)parts);   // (fewer than 2^28 units)
+        const int from = __builtin_amdgcn_readfirstlane((int)((unsigned)unit - tg * parts) * each), to = from + each < X.H ? from + each : X.H;
+        const Place at = Place::of<LPR>((long)tg * TPW, tokens, L);
         Turn turn;
-        turn.load(rt.cos, rt.sin, rt.at(token, t), rt.rot, rt.interleaved != 0, l, c, true);
+        turn.load(rt.cos, rt.sin, rt.at(at.token, at.t), rt.rot, rt.interleaved != 0, at.lane, at.c, true);
+        for (int h = from; h < to; h += U) {
+            Eight<T> y[U], x[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int h = h0 + u * HPW;
-            float dy[8], dyo[8], dz[8];
-            y[u].get(dy);
-            y[u].of_lane(turn.other).get(dyo);
-            turn.apply(dy, dyo, dz);
-            if (w) {
-                float a[8], ss = 0.f, gx = 0.f;
-                x[u].get(a);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    ss = __builtin_fmaf(a[e], a[e], ss);
-                    gx = __builtin_fmaf(dz[e] * f[e], a[e], gx);
+            for (int u = 0; u < U; ++u)
+                if (h + u < to) {
+                    y[u].load(at.row<const T>(Y, h + u));
+                    if (w) x[u].load(at.row<const T>(X, h + u));
                 }
-                ss = row_sum<LPR>(ss);
-                gx = row_sum<LPR>(gx);
-                const float r = 1.f / __builtin_sqrtf(ss * (1.f / D) + eps), k = r * r * (gx * (1.f / D));
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    dw[e] = __builtin_fmaf(dz[e] * r, a[e], dw[e]);
-                    dz[e] = r * (dz[e] * f[e] - a[e] * k);
+            for (int u = 0; u < U; ++u) {
+                if (h + u >= to) break;
+                float dy[8], dyo[8], dz[8];
+                y[u].get(dy);
+                y[u].of_lane(turn.other).get(dyo);
+                turn.apply(dy, dyo, dz);
+                if (w) {
+                    float a[8], f[8], ss = 0.f, gx = 0.f;
+                    x[u].get(a);
+                    wv.get(f);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        ss = __builtin_fmaf(a[e], a[e], ss);
+                        gx = __builtin_fmaf(dz[e] * f[e], a[e], gx);
+                    }
+                    ss = row_sum<LPR>(ss);
+                    gx = row_sum<LPR>(gx);
+                    const float r = 1.f / __builtin_sqrtf(ss * (1.f / D) + eps), k = r * r * (gx * (1.f / D)), rr = at.real ? r : 0.f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        dw[e] = __builtin_fmaf(dz[e] * rr, a[e], dw[e]);
+                        dz[e] = r * (dz[e] * f[e] - a[e] * k);
+                    }
                 }
-            }
-            if (h < X.H) {
                 y[u].set(dz);
-                y[u].store(static_cast<T *>(dX.data) + b * dX.batch + t * dX.token + h * dX.head + 8 * c);
+                if (at.real) y[u].store(at.row<T>(dX, h + u));
             }
         }
     }
@@ -160,9 +181,9 @@ __global__ __launch_bounds__(256) void k_norm_rotate_grad(HeadRows dQo, HeadRows
 #pragma unroll
         for (int o = 32; o >= LPR; o >>= 1) dw[e] += __shfl_xor(dw[e], o, kWave);
     }
-    if (g == 0) {
+    if (l < LPR) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sums[wave][8 * c + e] = dw[e];
+        for (int e = 0; e < 8; ++e) sums[wave][8 * l + e] = dw[e];
     }
     __syncthreads();
     if (threadIdx.x < D)
@@ -180,7 +201,13 @@ __global__ __launch_bounds__(256) void k_norm_weight_grad(const float *__restric
     const int from = blockIdx.y ? qgroups : 0, to = blockIdx.y ? groups : qgroups;
     const int col = threadIdx.x & 7, i = threadIdx.x >> 3;
     float s = 0.f;
-    for (int p = from + i; p < to; p += 32) s += part[(long)p * D + 8 * blockIdx.x + col];
+    for (int p = from + i; p < to; p += 8 * 32) {   // eight on their way at a time
+        float x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = part[(long)(p + 32 * k < to ? p + 32 * k : p) * D + 8 * blockIdx.x + col];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s += p + 32 * k < to ? x[k] : 0.f;
+    }
     sums[i][col] = s;
     __syncthreads();
 #pragma unroll
@@ -191,18 +218,24 @@ __global__ __launch_bounds__(256) void k_norm_weight_grad(const float *__restric
     if (i == 0) dw[8 * blockIdx.x + col] = sums[0][col];
 }
 
+// Heads that a wave goes through, for `groups` groups of tokens: as many as leave waves for the whole chip.
+int heads_each(long groups, int heads, long waves) {
+    long parts = (waves + groups - 1) / groups;
+    parts = parts < 1 ? 1 : parts > heads ? heads : parts;
+    return (int)((heads + parts - 1) / parts);
+}
+
 template <typename T, int D>
 hipError_t forward(const HeadRows &Q, const HeadRows &K, const void *wq, const void *wk, float eps, const RotaryTable &rt, long B,
                    int L, const HeadRows &Qo, const HeadRows &Ko, hipStream_t st) {
-    constexpr int HPW = 512 / D;
-    const long tokens = B * L;
-    const int heads = Q.H + K.H;
-    const int u = heads > 2 * HPW && tokens >= 512 ? 4 : heads > HPW && tokens >= 512 ? 2 : 1;
-    const long units = tokens * ((heads + HPW * u - 1) / (HPW * u));
-    const dim3 grid((unsigned)((units + 3) / 4));
+    constexpr int TPW = 512 / D;
+    const long tokens = B * L, groups = (tokens + TPW - 1) / TPW;
+    const int heads = Q.H + K.H, each = heads_each(groups, heads, kForwardWaves), parts = (heads + each - 1) / each;
+    const dim3 grid((unsigned)((groups * parts + 3) / 4));
 #define DFSS_LAUNCH(U)                                                                                                   \
-    hipLaunchKernelGGL((k_norm_rotate<T, D, U>), grid, dim3(256), 0, st, Q, K, (const T *)wq, (const T *)wk, eps, rt, tokens, L, Qo, Ko)
-    if (u == 4) DFSS_LAUNCH(4); else if (u == 2) DFSS_LAUNCH(2); else DFSS_LAUNCH(1);
+    hipLaunchKernelGGL((k_norm_rotate<T, D, U>), grid, dim3(256), 0, st, Q, K, (const T *)wq, (const T *)wk, eps, rt, tokens, L, \
+                       Qo, Ko, parts, each)
+    if (each >= 4) DFSS_LAUNCH(4); else DFSS_LAUNCH(1);
 #undef DFSS_LAUNCH
     return hipGetLastError();
 }
@@ -211,20 +244,19 @@ template <typename T, int D>
 hipError_t backward(const HeadRows &dQo, const HeadRows &dKo, const HeadRows &Q, const HeadRows &K, const void *wq, const void *wk,
                     float eps, const RotaryTable &rt, long B, int L, const HeadRows &dQ, const HeadRows &dK, float *dwq, float *dwk,
                     float *part, hipStream_t st) {
-    constexpr int HPW = 512 / D, U = 2;
-    const long tokens = B * L;
-    auto units = [&](int H) { return tokens * ((H + HPW * U - 1) / (HPW * U)); };
-    const long q = units(Q.H), k = K.H ? units(K.H) : 0;
+    constexpr int TPW = 512 / D, U = 1;
+    const long tokens = B * L, tg = (tokens + TPW - 1) / TPW;
+    const int each = heads_each(tg, Q.H + K.H, 4 * kGradGroups);
+    const long q = tg * ((Q.H + each - 1) / each), k = K.H ? tg * ((K.H + each - 1) / each) : 0;   // units
     long qg = (q + 3) / 4, kg = (k + 3) / 4;
     if (qg + kg > kGradGroups) {   // shared out by their work
-        long part_q = kGradGroups * q / (q + k);
-        if (part_q < 1) part_q = 1;
-        if (k && part_q > kGradGroups - 1) part_q = kGradGroups - 1;
-        qg = part_q;
-        kg = k ? kGradGroups - part_q : 0;
+        qg = kGradGroups * q / (q + k);
+        if (qg < 1) qg = 1;
+        if (k && qg > kGradGroups - 1) qg = kGradGroups - 1;
+        kg = k ? kGradGroups - qg : 0;
     }
     hipLaunchKernelGGL((k_norm_rotate_grad<T, D, U>), dim3((unsigned)(qg + kg)), dim3(256), 0, st, dQo, dKo, Q, K, (const T *)wq,
-                       (const T *)wk, eps, rt, tokens, L, dQ, dK, (int)qg, part);
+                       (const T *)wk, eps, rt, tokens, L, dQ, dK, (int)qg, each, part);
     if (wq || wk)
         hipLaunchKernelGGL((k_norm_weight_grad<D>), dim3(D / 8, 2), dim3(256), 0, st, part, (int)qg, (int)(qg + kg),
                            wq ? dwq : nullptr, wk ? dwk : nullptr);

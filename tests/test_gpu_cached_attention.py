@@ -52,6 +52,7 @@ APPENDS = [
     (32, 64, 5, [(31, 33), (1, 95), (0, 31), (0, 0)], True, 48, False),
     (128, 128, 2, [(100, 300), (0, 129), (127, 1)], True, 128, True),
     (128, 64, 2, [(130, 70), (0, 1)], False, 0, False),
+    (64, 128, 2, [(5, 60)] + [(10, 1)] * 69, True, 64, False),      # a prompt among single tokens
     (64, 64, 12, [(10, 3)] * 70, True, 64, False),          # more sequences than lanes
 ]
 

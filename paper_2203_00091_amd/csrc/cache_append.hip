@@ -234,18 +234,24 @@ hipError_t launch_cache_append(const HeadRows &K, const HeadRows &V, int T, cons
     // Rows that a call adds to a page, at most -- or, where the calls are those of a step of generation (about a token for each
     // sequence), most likely.  As few registers as those rows need: of many short units waves wait for memory one after the other.
     const int added = cu ? (T <= 2 * B ? 2 : T) : most, rows = page < added ? page : added, passes = (rows * (d / 8) + 63) / 64;
-    const bool wave = passes <= 8;
+    const bool wave = passes <= 4;
     // heads that a unit takes one after the other, its next rows on their way: as many as leave the chip full
     const long waves = (long)slots * 2 * c.Hk * (wave ? 1 : 4);
     const int each = waves >= 4 * kFullWaves ? 4 : waves >= 2 * kFullWaves ? 2 : 1, heads = each * (wave ? 4 : 1);
     const dim3 grid(slots, 2 * (unsigned)((c.Hk + heads - 1) / heads));
 #define DFSS_LAUNCH(D, WU, NP)                                                                                          \
     hipLaunchKernelGGL((k_cache_append<D, WU, NP>), grid, dim3(256), 0, st, K, V, T, cu, B, most, max_len, (const __bf16 *)w, eps, rt, c, each)
+    // 12k tokens x 1024 elements, us: one wave of eight passes 30.5 (d = 128, pages of 32) and 31.6 (64, 64), four of two 27.4 and
+    // 27.5; four waves of eight 33.5 (128, 64), of four 28.8.
+#define DFSS_PASSES(D)                                                                                                  \
+    if (passes <= 1) DFSS_LAUNCH(D, 1, 1); else if (passes <= 2) DFSS_LAUNCH(D, 1, 2); else if (passes <= 4) DFSS_LAUNCH(D, 1, 4); \
+    else if (passes <= 8) DFSS_LAUNCH(D, 4, 2); else if (passes <= 16) DFSS_LAUNCH(D, 4, 4); else DFSS_LAUNCH(D, 4, 8)
     if (d == 64) {
-        if (passes <= 1) DFSS_LAUNCH(64, 1, 1); else if (passes <= 2) DFSS_LAUNCH(64, 1, 2); else if (passes <= 4) DFSS_LAUNCH(64, 1, 4); else if (wave) DFSS_LAUNCH(64, 1, 8); else DFSS_LAUNCH(64, 4, 4);
+        DFSS_PASSES(64);
     } else {
-        if (passes <= 1) DFSS_LAUNCH(128, 1, 1); else if (passes <= 2) DFSS_LAUNCH(128, 1, 2); else if (passes <= 4) DFSS_LAUNCH(128, 1, 4); else if (wave) DFSS_LAUNCH(128, 1, 8); else DFSS_LAUNCH(128, 4, 8);
+        DFSS_PASSES(128);
     }
+#undef DFSS_PASSES
 #undef DFSS_LAUNCH
     return hipGetLastError();
 }

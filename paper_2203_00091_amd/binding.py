@@ -808,9 +808,12 @@ class Rotary:
         if len(shape) != 2:
             raise ValueError(f"cos, sin: expected [n_pos, rot/2], got {list(shape)}")
         self.cos, self.sin, self.pos, self.interleaved = cos, sin, pos, interleaved
-        p, self.device = _array(cos, f, shape, None, "cos"), cos.get_device()
-        self._c = _ROTARY.pack(p, _array(sin, f, shape, self.device, "sin"),
-                               0 if pos is None else _array(pos, torch.int32, pos.shape, self.device, "pos"), shape[0], 2 * shape[1], bool(interleaved))
+        self.device = dev = cos.get_device()
+        if not (_current(dev) and cos.dtype is f and sin.dtype is f and sin.shape == shape and sin.get_device() == dev
+                and cos.is_contiguous() and sin.is_contiguous()):
+            _array(cos, f, shape, None, "cos"), _array(sin, f, shape, dev, "sin")   # says what is wrong
+        self._c = _ROTARY.pack(cos.data_ptr(), sin.data_ptr(), 0 if pos is None else _array(pos, torch.int32, pos.shape, dev, "pos"),
+                               shape[0], 2 * shape[1], 1 if interleaved else 0)
 
 
 def _rotary(r: Rotary | None, tokens: int):
@@ -838,12 +841,19 @@ class Cache:
         self.k, self.v, self.k_scale, self.v_scale, self.table, self.len = k, v, k_scale, v_scale, table, len
         n, self.Hk, page, self.d = shape
         self.B, width = where
-        scales, codes = (n, self.Hk), k.dtype if k.dtype in _CODES else _CODES
-        p, dev = _array(k, codes, shape, None, "k"), k.get_device()
-        self.device = dev
-        self._c = _CACHE.pack(p, _array(v, codes, shape, dev, "v"), _array(k_scale, f, scales, dev, "k_scale"),
-                              _array(v_scale, f, scales, dev, "v_scale"), _array(table, i, where, dev, "table"),
-                              _array(len, i, where[:1], dev, "len"), n, self.Hk, page, width)
+        scales, codes, lens = (n, self.Hk), k.dtype, (self.B,)
+        self.device = dev = k.get_device()
+        if not (codes in _CODES and v.dtype is codes and k_scale.dtype is f and v_scale.dtype is f and table.dtype is i and len.dtype is i
+                and v.shape == shape and k_scale.shape == scales and v_scale.shape == scales and len.shape == lens
+                and _current(dev) and v.get_device() == dev and k_scale.get_device() == dev and v_scale.get_device() == dev
+                and table.get_device() == dev and len.get_device() == dev and k.is_contiguous() and v.is_contiguous()
+                and k_scale.is_contiguous() and v_scale.is_contiguous() and table.is_contiguous() and len.is_contiguous()):
+            # says what is wrong
+            _array(k, codes if codes in _CODES else _CODES, shape, None, "k"), _array(v, codes, shape, dev, "v")
+            _array(k_scale, f, scales, dev, "k_scale"), _array(v_scale, f, scales, dev, "v_scale")
+            _array(table, i, where, dev, "table"), _array(len, i, lens, dev, "len")
+        self._c = _CACHE.pack(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), table.data_ptr(), len.data_ptr(),
+                              n, self.Hk, page, width)
 
 
 def _rows(t: torch.Tensor | None, shape, dtype, what: str, out: bool = False):

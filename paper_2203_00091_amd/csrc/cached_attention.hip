@@ -139,7 +139,8 @@ __global__ __launch_bounds__(64 * NW, RT == 1 && D == 64 ? 3 : RT <= 2 ? 2 : 1) 
     // (scalar loads): the pages two blocks ahead, the scales one.
     constexpr int NG = BIG ? 1 : 4;
     struct Pages {
-        int id[NG], bad;      // page of each group (0 where there is none), and a bit for each 16 keys without one
+        long at[NG];          // page of each group (0 where there is none) * Hk + head
+        int bad;              // a bit for each 16 keys without one
     };
     struct Scales {
         float k[NG], v[NG];
@@ -152,7 +153,7 @@ __global__ __launch_bounds__(64 * NW, RT == 1 && D == 64 ? 3 : RT <= 2 ? 2 : 1) 
             const int entry = (jb * KB + 16 * g) >> cache.page_shift;
             const int id = scalar_load(my_table, entry < last_entry ? entry : last_entry);
             const bool none = (unsigned)id >= (unsigned)cache.n_pages;
-            p.id[g] = none ? 0 : id;
+            p.at[g] = (long)(none ? 0 : id) * cache.Hk + R.h;
             p.bad |= none ? (BIG ? 15 : 1 << g) : 0;
         }
         return p;
@@ -161,14 +162,14 @@ __global__ __launch_bounds__(64 * NW, RT == 1 && D == 64 ? 3 : RT <= 2 ? 2 : 1) 
         Scales s;
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-            const long at = (long)p.id[g] * cache.Hk + R.h;
-            s.k[g] = scalar_load(Ks, at);
-            s.v[g] = scalar_load(Vs, at);
+            s.k[g] = scalar_load(Ks, p.at[g]);
+            s.v[g] = scalar_load(Vs, p.at[g]);
         }
         return s;
     };
+    const int place_shift = cache.page_shift + (D == 64 ? 6 : 7);
     auto place = [&](const Pages &p, int jb, int g) {   // bytes before a group's first key
-        return ((((long)p.id[g] * cache.Hk + R.h) << cache.page_shift) + ((jb * KB + 16 * g) & page_mask)) * D;
+        return (p.at[g] << place_shift) + ((jb * KB + 16 * g) & page_mask) * D;
     };
     auto pick = [](bool second, auto x, auto y) { return second ? y : x; };   // (by value: of an array it would be a load)
     constexpr int G1 = BIG ? 0 : 1, G2 = BIG ? 0 : 2, G3 = BIG ? 0 : 3;

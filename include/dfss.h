@@ -448,7 +448,8 @@ dfss_status dfss_qk_norm_rotate_backward(const dfss_rows *dQo, const dfss_rows *
  * [n_pages, Hk, page, d] and for every page and head one scale, a power of two; a code stands for its e4m3 value times
  * the scale.  Token i of sequence b lies in row i % page of page table[b][i / page].  len[b]: tokens of the
  * sequence.  Page numbers outside [0, n_pages) are no pages: tokens of theirs are not kept, and no query
- * sees them.  Entries of the table behind a sequence's last token are not read. */
+ * sees them.  Entries of the table behind a sequence's last token are not read.  The pages that a sequence's
+ * entries name are different ones.  Scales are powers of two (dfss_cache_append makes no others). */
 typedef struct {
     void *k, *v;              /* device, uint8, 16-byte aligned                                          */
     void *k_scale, *v_scale;  /* device, float32 [n_pages, Hk], 4-byte aligned                           */

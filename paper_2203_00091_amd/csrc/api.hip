@@ -735,7 +735,7 @@ dfss_status cache_of(const dfss_cache *c, const dfss_shape *s, dfss::PagedCache 
     if (!c || !s) return DFSS_ERR_NULL;
     if (!c->k || !c->v || !c->k_scale || !c->v_scale || !c->table || !c->len) return DFSS_ERR_NULL;
     if (s->B <= 0 || s->H <= 0 || s->Lq <= 0 || s->Lk <= 0 || s->d <= 0) return DFSS_ERR_SHAPE;
-    if (c->n_pages <= 0 || c->Hk <= 0 || c->Hk > 65535 || c->width <= 0) return DFSS_ERR_SHAPE;
+    if (c->n_pages <= 0 || c->Hk <= 0 || c->Hk > 32767 || c->width <= 0) return DFSS_ERR_SHAPE;
     if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return DFSS_ERR_SHAPE;
     if (s->B > (1 << 20) || s->Lq > (1 << 24) || s->Lk > (1 << 24) || (int64_t)c->width * c->page < s->Lk) return DFSS_ERR_SHAPE;
     if (s->dtype != DFSS_BF16) return DFSS_ERR_UNSUPPORTED;

@@ -455,8 +455,11 @@ __global__ __launch_bounds__(2 * D) void k_cached_merge(const float *__restrict_
         pack_bf16x2(a0[0], a0[1]), pack_bf16x2(a0[2], a0[3]), pack_bf16x2(a1[0], a1[1]), pack_bf16x2(a1[2], a1[3])};
 }
 
-// 16-row tiles of a workgroup
-int row_tiles(long rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : kWide; }
+// 16-row tiles of a workgroup.  32 sequences of up to 4096 keys, us, in tiles of 32 rows and of 128 (cached_wide.hip):
+//   8 key heads, d = 128, pages of 64, 2:4     48 rows 63 and 76, 64 rows 65 and 82, 96 rows 96 and 81, 256 rows 187 and 150
+//   16 key heads, d = 64, pages of 32, full    48 rows 66 and 118, 96 rows 81 and 122, 128 rows 106 and 123, 192 rows 145 and 213
+// and at d = 64 with 2048 rows, 2:4, 2 x 16 heads 150 and 109.
+int row_tiles(long rows, int d) { return rows <= 16 ? 1 : rows <= (d == 64 ? 128 : 64) ? 2 : kWide; }
 
 struct Plan {
     int RT, NW, tiles, target, least;   // NW: waves of a workgroup; target 0: nobody shares
@@ -464,7 +467,7 @@ struct Plan {
 Plan plan(int B, int Hk, int G, int most, int max_len, int d) {
     Plan p;
     const long rows = (long)most * G;
-    p.RT = row_tiles(rows);
+    p.RT = row_tiles(rows, d);
     p.tiles = (int)((rows + 16 * p.RT - 1) / (16 * p.RT));
     const long per_share = (long)Hk * p.tiles, items = B * per_share;   // workgroups of a share, and without shares
     const int blocks = (max_len + KB - 1) / KB;

@@ -9,7 +9,7 @@
 //
 // Scores, selection and products are those of k_fused32 (fused_attention32.hip): 32 x 32 tiles, scores relative to the softmax
 // reference c from the accumulator on, the position of a score in its two lowest bits.  Hidden keys have the score -1e30; a query that has
-// seen no key yet has no reference (c = 0, and nothing it adds up counts).  c is a whole number, so that scores of whole numbers stay exact.
+// seen no key yet has no reference (c = 0, and nothing it adds up counts).
 // With 16 x 16 tiles and exact comparisons 97 us, so 82.  What bounds it then is the rate at which two waves of a SIMD unit issue: about 540
 // instructions a block and wave.  (Level: the tiles of the first product in turn, more operands ahead, the teams in step.)
 #include <math.h>
@@ -24,7 +24,9 @@ namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr float kTau = 4.0f;    // distance of the reference above the row maximum it was set from (in scaled scores)
+// Distance of the reference above the row maximum that it was set from, in scaled scores; in raw ones at most kMostTau, whatever the
+// scale: scores are rounded at the magnitude of s' = q . k - c, and the comparison has to tell raw scores apart.
+constexpr float kTau = 4.0f, kMostTau = 64.0f;
 constexpr float kHidden = -1.0e30f;
 
 __device__ __forceinline__ float with_position(float v, uint32_t pos) {
@@ -176,8 +178,13 @@ __global__ __launch_bounds__(512, 2) void k_cached_wide(const __bf16 *__restrict
         }
     };
     const float k2 = sz.c;                                   // weight = exp2(s' k2)
-    const float tau = kTau * 1.4426950408889634f / sz.c;     // kTau in units of the raw dot product
-    float cref = 0.f;                                        // reference of query lj (raw dot product; a whole number)
+    const float tau = fminf(kTau * 1.4426950408889634f / sz.c, kMostTau);   // in units of the raw dot product
+    // References are multiples of a power of two: of 1, so that scores of whole numbers stay exact, or less where a whole number is much
+    // to a scaled score (a reference far above the scores would leave weights of 0 only).
+    int above = (int)(__float_as_uint(sz.c) >> 23) - 126;
+    above = above < 100 ? above : 100;
+    const float unit = __uint_as_float((uint32_t)(above > 0 ? 127 - above : 127) << 23), per_unit = __uint_as_float((uint32_t)(above > 0 ? 127 + above : 127) << 23);
+    float cref = 0.f;                                        // reference of query lj (raw dot product)
     bool unset = true;                                       // it has none yet
     f32x16 cneg, acc_o[DT], acc_l;                           // -cref, from which the score tiles start
 #pragma unroll
@@ -192,6 +199,7 @@ __global__ __launch_bounds__(512, 2) void k_cached_wide(const __bf16 *__restrict
     const int tr_colgrp = (l >> 4) & 1;   // which 16 of the 32 columns of a tile this lane group reads
 
     Fetched f;
+    f.bad = 0;
     Pages ahead;                 // of the block that is fetched next (asked for a step ahead)
     int bad = 0;                 // groups without a page of this block
     const int mine = begin + team;
@@ -246,7 +254,7 @@ __global__ __launch_bounds__(512, 2) void k_cached_wide(const __bf16 *__restrict
             }
             float kept[2][2 * NP];
             uint32_t idx = 0;       // positions: tile 0 in the low half
-            for (;;) {
+            for (int pass = 0; pass < 3; ++pass) {   // (two do; with scores that are no numbers, as many as this)
                 float m_blk = -3.0e38f;
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
@@ -275,8 +283,10 @@ __global__ __launch_bounds__(512, 2) void k_cached_wide(const __bf16 *__restrict
                 if (!__any(m_blk >= least)) break;
                 const float mq = fmaxf(m_blk, __shfl_xor(m_blk, 32, 64));   // lanes lj and lj + 32 hold different keys of the same query
                 const bool up = mq >= least;
-                // (whole and above the row maximum by tau or more: after this pass every score of the block is negative, and the loop ends)
-                const float c_new = up ? __builtin_ceilf(cref + mq + tau) : cref, delta = c_new - cref;
+                // (above the row maximum by more than its rounding: after this pass every score of the block is negative)
+                const float most = cref + mq + tau;
+                const float c_new = up ? (__builtin_ceilf((most + 0x1p-22f * __builtin_fabsf(most)) * per_unit) + 1.f) * unit : cref;
+                const float delta = c_new - cref;
                 const float alpha = up && !unset ? __builtin_amdgcn_exp2f(-delta * k2) : 1.f;
                 cref = c_new;
                 unset = unset && !up;

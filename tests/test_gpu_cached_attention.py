@@ -214,9 +214,10 @@ class Attend:
         clear = gap > 1e-4 * (0 if all_rows else 1)     # a choice by less than 32 bits of the scores hold may go either way
         assert float(clear.double().mean()) > 0.9 or want.numel() < 2000
         # O is rounded to bfloat16, and so is every weight, in the sum as in the product: half a step of |O| for the first,
-        # half a step of sum p |v| and of |O| for the second; 1e-5 for 32-bit sums and exponentials
+        # half a step of sum p |v| and of |O| for the second; 1e-5 for 32-bit sums and exponentials; weights below 2^-126, the
+        # least normal number, are 0: 10000 keys x 2^-126 x |v| <= 448 is 6e-32
         half = torch.finfo(torch.bfloat16).eps / 2
-        tol = half * want.abs() + (half + 1e-5) * (amount + want.abs()) * 1.01
+        tol = half * want.abs() + (half + 1e-5) * (amount + want.abs()) * 1.01 + 6e-32
         off = ((O.cpu().double() - want).abs() - tol)[clear]
         assert bool(O.isfinite().all())
         assert off.numel() == 0 or float(off.max()) <= 0
@@ -301,6 +302,17 @@ def test_scores_far_apart(mode):
     """A few keys carry all the weight; the reference is raised again and again."""
     a = Attend(64, 16, 1, 4, [(400, 1), (1000, 5)], 41, size=8.0)
     a.check(a.call(*mode), *mode)
+
+
+@pytest.mark.parametrize("mode", MODES, ids=str)
+@pytest.mark.parametrize("scale", [2.0 ** -14, 1.0, 64.0])
+@pytest.mark.parametrize("queries", [1, 100])
+def test_any_scale(queries, scale, mode):
+    """Nearly equal weights, and one key with all of it: equal scores are exact ones of whole numbers."""
+    for d, page in ((64, 64), (128, 16)):
+        a = Attend(d, page, 1, 4, [(300, queries), (130, queries)], 47, integers=True)
+        a.scale = scale
+        a.check(a.call(*mode), *mode, all_rows=True)
 
 
 def test_rows_of_no_sequence_stay():

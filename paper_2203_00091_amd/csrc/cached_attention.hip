@@ -80,7 +80,7 @@ __device__ __forceinline__ void weigh(const f32x4 (&s)[4], float c, int kb, bf16
 
 // BIG: pages of 64 tokens or more, a block lies in one.
 template <int D, int MODE, int NW, int RT, bool BIG>
-__global__ __launch_bounds__(64 * NW, RT == 1 && D == 64 ? 3 : RT <= 2 ? 2 : 1) void k_cached(const __bf16 *__restrict__ Q, const int *__restrict__ cu, PagedCache cache,
+__global__ __launch_bounds__(64 * NW, NW == 16 ? 4 : RT == 1 && D == 64 ? 3 : RT <= 2 ? 2 : 1) void k_cached(const __bf16 *__restrict__ Q, const int *__restrict__ cu, PagedCache cache,
                                                     const uint8_t *__restrict__ Kc, const uint8_t *__restrict__ Vc,
                                                     const float *__restrict__ Ks, const float *__restrict__ Vs,
                                                     const int *__restrict__ table, Sizes sz, uint16_t *__restrict__ O,
@@ -474,6 +474,10 @@ Plan plan(int B, int Hk, int G, int most, int max_len, int d) {
     p.NW = items <= 256 || p.RT == kWide ? 8 : 4;
     p.target = 0;
     p.least = p.NW;
+    // d = 64: sixteen waves walk 80 blocks before a second kernel pays.  12 heads a sequence, 4096 keys, us, sixteen waves, and eight
+    // that share the keys with others: 1 sequence 12.7 and 6.1 + 5, 8 of them 14.3 and 13.3 + 5, 20 21.0 and 29.7 + 5; eight waves are
+    // enough up to 40 blocks (2000 keys: 9.5 and 9.2).
+    if (d == 64 && p.RT == 1 && items <= 256 && blocks > 40 && blocks <= 80) p.NW = 16;
     if (blocks <= 5 * p.NW || (long)B * blocks > 1 << 30) return p;
     if (items * blocks <= 4096 && p.RT != kWide) p.NW = 4;
     const long slots = p.NW == 8 ? 256 : 512;
@@ -503,7 +507,7 @@ hipError_t launch(const HeadRows &Q, int T, const int *cu, int B, int most, int 
     if (p.RT == kWide) {
         if (const hipError_t e = launch_wide((const __bf16 *)Q.data, cu, c, D, MODE, sz, p.target ? shares : items, (uint16_t *)O, part, st)) return e;
     } else if (p.RT == 1) {
-        if (p.NW == 8) { DFSS_PAGES(8, 1); } else { DFSS_PAGES(4, 1); }
+        if (p.NW == 16) { if constexpr (D == 64) { DFSS_PAGES(16, 1); } } else if (p.NW == 8) { DFSS_PAGES(8, 1); } else { DFSS_PAGES(4, 1); }
     } else {
         if (p.NW == 8) { DFSS_PAGES(8, 2); } else { DFSS_PAGES(4, 2); }
     }

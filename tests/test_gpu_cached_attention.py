@@ -419,3 +419,26 @@ def test_another_stream():
         got = a.call(2, 4)
     torch.cuda.current_stream().wait_stream(side)
     assert torch.equal(got, want)
+
+
+def test_pages_behind_four_gigabytes():
+    """Places in a cache that 32 bits do not hold: the same tokens in the first and in the last pages."""
+    page, Hk, d = 128, 8, 128
+    n_pages = (1 << 32) // (page * Hk * d) + 16
+    free, _ = torch.cuda.mem_get_info()
+    if free < 3 * n_pages * page * Hk * d:
+        pytest.skip("too little memory")
+    k, v = (torch.empty((n_pages, Hk, page, d), dtype=torch.uint8, device=DEV) for _ in range(2))
+    k_scale, v_scale = (torch.empty((n_pages, Hk), device=DEV) for _ in range(2))
+    length = torch.tensor([300, 300], dtype=torch.int32, device=DEV)
+    table = torch.tensor([[2, 0, 1], [n_pages - 2, n_pages - 1, n_pages - 3]], dtype=torch.int32, device=DEV)
+    cache = Cache(k, v, k_scale, v_scale, table, length)
+    g = torch.Generator().manual_seed(48)
+    rows = torch.randn((300, 2 * Hk, d), generator=g).bfloat16().to(DEV).repeat(2, 1, 1)
+    dfss.dfss_cache_append(rows[:, :Hk], rows[:, Hk:], None, cache, None, None, Shape(2, Hk, 300, 300, d))
+    assert torch.equal(k[table[0, 2].item(), :, :44], k[table[1, 2].item(), :, :44]) and torch.equal(v[table[0, 0].item()], v[table[1, 0].item()])
+    for queries in (1, 130):
+        Q = torch.randn((queries, 2 * Hk, d), generator=g).bfloat16().to(DEV).repeat(2, 1, 1)
+        for f in (dfss.dfss_attention_cached, dfss.dense_attention_cached):
+            O = f(Q, None, cache, Shape(2, 2 * Hk, queries, 300, d, 2, 4), d ** -0.5)
+            assert torch.equal(O[:queries], O[queries:]) and bool(O.isfinite().all()) and O.any()

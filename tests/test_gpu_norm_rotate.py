@@ -185,3 +185,32 @@ def test_captured_and_on_another_stream():
         eager = list(s.forward()) + list(s.backward())
         assert all(torch.equal(a, b) for a, b in zip(list(out) + list(back), eager))
     assert all(torch.equal(a, b) for a, b in zip(list(out) + list(back), list(want) + list(grads)))
+
+
+def test_strides_that_32_bits_do_not_hold():
+    far = (1 << 31) + 64
+    if torch.cuda.mem_get_info()[0] < 3 * 2 * far:
+        pytest.skip("too little memory")
+    buffer = torch.empty(far + 4096, dtype=torch.bfloat16, device=DEV)
+    Q = buffer.as_strided((2, 3, 2, 64), (far, 128, 64, 1))
+    x = torch.randn((2, 3, 2, 64), generator=torch.Generator().manual_seed(18)).bfloat16().to(DEV)
+    Q.copy_(x)
+    w = torch.ones(64, dtype=torch.bfloat16, device=DEV)
+    s = Shape(2, 2, 3, 3, 64, 1, 2)
+    want, _ = dfss.dfss_qk_norm_rotate(x, None, w, None, None, s)
+    got, _ = dfss.dfss_qk_norm_rotate(Q, None, w, None, None, s)
+    assert torch.equal(got, want)
+    dfss.dfss_qk_norm_rotate(x, None, w, None, None, s, Qo=Q)
+    assert torch.equal(Q.transpose(1, 2).reshape(4, 3, 64), want)
+
+
+def test_many_tokens_and_heads():
+    """Every element against the same rows in another shape: more waves than the chip holds, and fewer."""
+    x = torch.randn((4, 1500, 24, 64), generator=torch.Generator().manual_seed(19)).bfloat16().to(DEV)
+    w = torch.ones(64, dtype=torch.bfloat16, device=DEV)
+    cos, sin = (t.to(DEV) for t in _angles(1500, 64))
+    whole, _ = dfss.dfss_qk_norm_rotate(x, None, w, None, Rotary(cos, sin), Shape(4, 24, 1500, 1500, 64, 1, 2))
+    for b, t, h in ((0, 0, 0), (3, 1499, 23), (1, 777, 5)):
+        at = torch.tensor([[t]], dtype=torch.int32, device=DEV)
+        one, _ = dfss.dfss_qk_norm_rotate(x[b:b + 1, t:t + 1, h:h + 1], None, w, None, Rotary(cos, sin, at), Shape(1, 1, 1, 1, 64, 1, 2))
+        assert torch.equal(one[0, 0], whole.view(4, 24, 1500, 64)[b, h, t])

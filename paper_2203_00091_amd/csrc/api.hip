@@ -694,6 +694,12 @@ dfss_status rotary_of(const dfss_rotary *r, int d, dfss::RotaryTable *out) {
     return DFSS_OK;
 }
 
+// of the calls over a cache: between 2^-100 and 2^100, with which hidden scores weigh 0 and a reference stays a number
+inline bool bad_cached_scale(float x) {
+    uint32_t u;
+    memcpy(&u, &x, sizeof(u));
+    return u < (127u - 100) << 23 || u > (127u + 100) << 23;
+}
 // eps: finite and >= 0 (on the bit pattern, as bad_scale)
 inline bool bad_eps(float x) {
     uint32_t u;
@@ -769,7 +775,7 @@ dfss_status attention_cached(const dfss_rows *Q, int32_t rows, const int32_t *cu
         else if (s->N == 1 && s->M == 2) mode = 1;
         else return DFSS_ERR_UNSUPPORTED;
     }
-    if (bad_scale(scale)) return DFSS_ERR_UNSUPPORTED;
+    if (bad_cached_scale(scale)) return DFSS_ERR_UNSUPPORTED;
     if (dfss_status st = rows_of(Q, 2, &R)) return st;
     if (rows <= 0 || rows > (1 << 27) || R.H != s->H || misaligned(O) || misaligned_to(cu, 4)) return DFSS_ERR_SHAPE;
     if (!cu && (long long)s->B * s->Lq != rows) return DFSS_ERR_SHAPE;

@@ -14,8 +14,17 @@
 // v_cvt_scalef32_pk_bf16_fp8 turns a pair of codes into bfloat16 times the scale, exactly: a code has 4 significant bits
 // and the scale is a power of two.  The weights are rounded to bfloat16 for the second product, and summed as rounded.
 //
+// K and V of one block only: with registers for two, half as many waves fit, and 64 sequences of up to 4096 keys took 127 us, so 83.
+//
 // The keys of a row tile go to the NW waves of a workgroup, and to several workgroups where the tiles are few or the
 // sequences long; partial results (reference, sum, unnormalised O, fp32) are merged in a fixed order.
+//
+// Measured, one query a sequence (bytes of the codes that the lengths reach; a copy of 1 GiB runs at 5.1 TB/s, a sum over it at 4.0):
+//   64 sequences of up to 4096 keys, 32 heads on 8, d = 128, pages of 16, 2:4      404 MB   81 us   5.0 TB/s
+//   128 of up to 2048, 16 heads on 16, d = 64, pages of 32, full                   404 MB   77 us   5.2 TB/s
+//   4 of up to 32768, 32 heads on 8, d = 128, pages of 128, full                   201 MB   42 + 5 (merge) us   4.9 TB/s
+//   24 of up to 2500, four queries, 12 heads on 4, d = 64, pages of 32, 1:2         23 MB   12.4 us: five blocks a wave, one after the other
+//   1 of 4096, 12 heads on 12, d = 64, pages of 64, 2:4                              6 MB   13.2 us: the same, four blocks a wave
 #include <math.h>
 
 #include <type_traits>
@@ -65,7 +74,7 @@ __device__ __forceinline__ void weigh(const f32x4 (&s)[4], float c, int kb, bf16
             for (int t = 0; t < DT; ++t) acc_o[t][r] *= a_r;
         }
     }
-    const float mb = m_ref * c;
+    const float mb = fmaxf(m_ref * c, -1.0e37f);   // (no infinity while there is no reference: -inf + inf is no weight)
 #pragma unroll
     for (int y = 0; y < NP / 8; ++y) {
         u32x4 pk;
@@ -471,6 +480,9 @@ Plan plan(int B, int Hk, int G, int most, int max_len, int d) {
     p.tiles = (int)((rows + 16 * p.RT - 1) / (16 * p.RT));
     const long per_share = (long)Hk * p.tiles, items = B * per_share;   // workgroups of a share, and without shares
     const int blocks = (max_len + KB - 1) / KB;
+    // Eight waves where that is still one workgroup for each compute unit at most: the wave's own chain of blocks sets the time there
+    // (4 sequences of 32768 keys, 8 key heads, d = 128, shared: 42 + 5 us, with four waves 48 + 8).  Four where workgroups follow each
+    // other, since a new one then starts sooner (128 sequences of 2048 keys, 16 heads, d = 64: 77, with eight 87).
     p.NW = items <= 256 || p.RT == kWide ? 8 : 4;
     p.target = 0;
     p.least = p.NW;
@@ -478,8 +490,14 @@ Plan plan(int B, int Hk, int G, int most, int max_len, int d) {
     // that share the keys with others: 1 sequence 12.7 and 6.1 + 5, 8 of them 14.3 and 13.3 + 5, 20 21.0 and 29.7 + 5; eight waves are
     // enough up to 40 blocks (2000 keys: 9.5 and 9.2).
     if (d == 64 && p.RT == 1 && items <= 256 && blocks > 40 && blocks <= 80) p.NW = 16;
+    // Five blocks a wave cost less than a second kernel, 5 us (24 sequences of 2500 keys, 4 key heads, d = 64: 12.4 alone, 11.9 + 4.6
+    // shared).  (Behind 2^30 the sum of blocks that the shares are counted in would pass 32 bits.)
     if (blocks <= 5 * p.NW || (long)B * blocks > 1 << 30) return p;
+    // Few blocks in all: shares of four blocks, so that there are twice as many of them.
     if (items * blocks <= 4096 && p.RT != kWide) p.NW = 4;
+    // Workgroups that the chip holds at a time, by their registers and LDS.  Where the sequences alone are that many, sharing only
+    // evens their lengths out, which is worth the merge for long ones alone (64 sequences of up to 4096 keys, 8 key heads, d = 128:
+    // 81 us alone, 96 + 6 shared), and with four rounds of them lengths even out by themselves.
     const long slots = p.NW == 8 ? 256 : 512;
     if (items >= 4 * slots || (items >= slots && blocks < 128)) return p;
     p.least = p.NW;

@@ -8,9 +8,9 @@
 // block's codes are in registers while this one is worked on, those after it on their way; one barrier a block.
 //
 // Scores, selection and products are those of k_fused32 (fused_attention32.hip): 32 x 32 tiles, scores relative to the softmax
-// reference c from the accumulator on, the position of a score in its two lowest bits.  Hidden keys have the score -1e30; a query that has
+// reference c from the accumulator on, the position of a score in its two lowest bits.  Hidden keys have the score -3e38; a query that has
 // seen no key yet has no reference (c = 0, and nothing it adds up counts).
-// With 16 x 16 tiles and exact comparisons 97 us, so 82.  What bounds it then is the rate at which two waves of a SIMD unit issue: about 540
+// With 16 x 16 tiles and exact comparisons 97 us, so 82 (of 22 at the rate of a large matrix product).  What bounds it then is the rate at which two waves of a SIMD unit issue: about 540
 // instructions a block and wave.  (Level: the tiles of the first product in turn, more operands ahead, the teams in step.)
 #include <math.h>
 
@@ -27,7 +27,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 // Distance of the reference above the row maximum that it was set from, in scaled scores; in raw ones at most kMostTau, whatever the
 // scale: scores are rounded at the magnitude of s' = q . k - c, and the comparison has to tell raw scores apart.
 constexpr float kTau = 4.0f, kMostTau = 64.0f;
-constexpr float kHidden = -1.0e30f;
+constexpr float kHidden = -3.0e38f;
 
 __device__ __forceinline__ float with_position(float v, uint32_t pos) {
     return __uint_as_float((__float_as_uint(v) & 0xFFFFFFFCu) | pos);

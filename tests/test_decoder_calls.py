@@ -119,7 +119,7 @@ def test_attention_refuses(host):
             assert call(dense, cache=host.cache(**kw)) == want, kw
         assert call(dense, Q=host.rows(H=3), shape=Shape(3, 3, 5, 256, 64)) == SHAPE      # no whole group of heads
         assert call(dense, Q=host.rows(H=2)) == SHAPE and call(dense, rows=0) == SHAPE and call(dense, cu=None, rows=16) == SHAPE
-        for scale in (0.0, -1.0, float("nan"), float("inf")):
+        for scale in (0.0, -1.0, float("nan"), float("inf"), 2.0 ** -101, 2.0 ** 101, 1e-40):
             assert call(dense, scale=scale) == UNSUP
         for bad, want in ((Shape(3, 4, 5, 256, 96), UNSUP), (Shape(3, 4, 5, 256, 64, 1, 2, dfss.DFSS_F32_BF16X3), UNSUP), (Shape(3, 4, 5, 300, 64), SHAPE),
                           (Shape(1 << 10, 4, 1 << 20, 256, 64), SHAPE)):

@@ -315,6 +315,17 @@ def test_any_scale(queries, scale, mode):
         a.check(a.call(*mode), *mode, all_rows=True)
 
 
+@pytest.mark.parametrize("mode", MODES, ids=str)
+@pytest.mark.parametrize("scale, size", [(2.0 ** -100, 1.0), (2.0 ** 100, 2.0 ** -102)])
+@pytest.mark.parametrize("queries", [1, 100])
+def test_the_least_and_largest_scales(queries, scale, size, mode):
+    """Level weights of what is seen and none of what is hidden; and scaled scores as usual from very small ones."""
+    for d, page in ((64, 64), (128, 16)):
+        a = Attend(d, page, 1, 4, [(300, queries), (130, queries), (2, 1)], 49, integers=True)
+        a.scale, a.Q = scale, a.Q * size
+        a.check(a.call(*mode), *mode, all_rows=True)
+
+
 def test_rows_of_no_sequence_stay():
     a = Attend(64, 16, 1, 2, [(50, 3), (20, 1)], 42)
     a.Q = torch.cat((a.Q, a.Q))

@@ -315,6 +315,10 @@ __global__ __launch_bounds__(64 * NW, NW == 16 ? 4 : RT == 1 && D == 64 ? 3 : RT
 #pragma unroll
                         for (int x = 0; x < VW; ++x) vr[st][e][x] = 0u;
                 }
+            // (nor is the scale of the page that was read in place of none)
+#pragma unroll
+            for (int st = 0; st < 2; ++st)
+                if (bad >> (2 * st + v_group) & 1) v_s[st] = 1.f;
         }
         bf16x8 p[RT][DENSE ? 2 : 1];
         uint32_t idx[RT];

@@ -153,6 +153,8 @@ __global__ __launch_bounds__(512, 2) void k_cached_wide(const __bf16 *__restrict
             for (int i = 0; i < PIECES; ++i) {
                 const int key = (64 / PIECES) * i + f_key;
                 if (jb * KB + key >= R.keys || (f.bad >> (key >> 4) & 1)) f.v[i] = u32x4{0u, 0u, 0u, 0u};
+                // (nor is the scale of the page that was read in place of none; the group of the wave's keys, as in fetch)
+                if (f.bad >> ((64 / LPK * w + 64 / PIECES * i) >> 4) & 1) f.vs[i] = 1.f;
             }
         }
 #pragma unroll

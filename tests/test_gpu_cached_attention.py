@@ -287,6 +287,28 @@ def test_rows_that_see_nothing(mode):
 
 
 @pytest.mark.parametrize("mode", MODES, ids=str)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("queries", [1, 4, 70])
+def test_pages_that_are_none_and_a_page_nobody_names(queries, page, d, mode):
+    """Rows of every size of tile, the first of them before the first key; what lies in a page that no sequence names, its
+    scales included, is nobody's."""
+    a = Attend(d, page, 2, 5, [(0, queries), (queries // 2 + 1, queries), (260, queries), (130, 1), (-3, 1)], 50,
+               bad=[(2, 0), (2, 2), (2, 3), (3, 1)])
+    spare = next(i for i in range(1, a.k.shape[0]) if not bool((a.table == i).any()))
+    for x in (a.k, a.v, a.k_scale, a.v_scale):
+        x[spare] = x[0]
+    a.table[a.table == 0] = spare
+    want = a.reference(*mode)[0]
+    a.check(O := a.call(*mode), *mode)      # (the cache on the device is as it was, with page 0 in its place)
+    for x in (a.k, a.v):
+        x[0] = 0x7F                         # no number
+    a.k_scale[0], a.v_scale[0] = math.inf, math.nan
+    a.cache = Cache(*(x.to(DEV) for x in (a.k, a.v, a.k_scale, a.v_scale)), a.table.to(DEV), a.cache.len)
+    assert torch.equal(a.reference(*mode)[0], want) and torch.equal(a.call(*mode), O)
+
+
+@pytest.mark.parametrize("mode", MODES, ids=str)
 def test_the_call_sees_no_more_keys_than_it_names(mode):
     a = Attend(64, 32, 2, 1, [(200, 1), (90, 1), (150, 1)], 39, uniform=True)
     a.check(a.call(*mode, causal=False, max_len=100), *mode, causal=False, max_len=100)

@@ -856,6 +856,14 @@ class Cache:
                               n, self.Hk, page, width)
 
 
+def _scratch(ws: torch.Tensor | None) -> int | None:
+    """Pointer of a workspace of the caller's."""
+    p = _ptr(ws)
+    if ws is not None and not _current(ws.get_device()):
+        raise ValueError(f"ws: expected a tensor on the current device, got one on {ws.device}")
+    return p
+
+
 def _rows(t: torch.Tensor | None, shape, dtype, what: str, out: bool = False):
     """Rows of heads, as bytes, and their number of heads (None, 0 without a tensor): [batch, token, head, d] with any strides of the first
     three, or the contiguous [batch * head, token, d] of the attention calls, for a shape (batch, token, d); [token, head, d]
@@ -870,7 +878,7 @@ def _rows(t: torch.Tensor | None, shape, dtype, what: str, out: bool = False):
             raise ValueError(f"{what}: expected [{shape[0]}, heads, {d}] with elements side by side, got {list(n)}")
         H, batch, token, head = n[1], 0, x[0] if n[0] > 1 else 0, x[1] if n[1] > 1 else 0
     elif dims == 3:
-        if n[0] % shape[0] or n[1] != shape[1] or n[2] != d or not t.is_contiguous():
+        if shape[0] < 1 or n[0] % shape[0] or n[1] != shape[1] or n[2] != d or not t.is_contiguous():
             raise ValueError(f"{what}: expected a contiguous [{shape[0]} * heads, {shape[1]}, {d}], got {list(n)}")
         H = n[0] // shape[0]
         batch, token, head = H * shape[1] * d, d, shape[1] * d
@@ -938,7 +946,7 @@ def dfss_qk_norm_rotate_backward(dQo, dKo, Q, K, wq, wk, rotary: Rotary | None, 
     st = load_library().dfss_qk_norm_rotate_backward(
         _rows(dQo, shape, t, "dQo")[0], _rows(dKo, shape, t, "dKo")[0], q, k, _weight(wq, t, s.d, "wq"), _weight(wk, t, s.d, "wk"),
         _rotary(rotary, s.B * s.Lq), s._call.ref, eps, _rows(dQ, shape, t, "dQ", True)[0], _rows(dK, shape, t, "dK", True)[0],
-        _weight(dwq, torch.float32, s.d, "dwq"), _weight(dwk, torch.float32, s.d, "dwk"), _ptr(ws),
+        _weight(dwq, torch.float32, s.d, "dwq"), _weight(dwk, torch.float32, s.d, "dwk"), _scratch(ws),
         0 if ws is None else ws.numel() * ws.element_size(), _stream())
     _check("dfss_qk_norm_rotate_backward", st)
     return dQ, dK, dwq, dwk
@@ -982,7 +990,7 @@ def _attention_cached(name: str, Q, cu, cache: Cache, s: Shape, scale: float, ca
     L = load_library()
     w = None
     if ws is not None:
-        need, w = ws.numel() * ws.element_size(), _ptr(ws)
+        need, w = ws.numel() * ws.element_size(), _scratch(ws)
     else:
         need = s._call.cached_ws.get(cache.Hk)      # (of a valid shape it depends on nothing else of the cache)
         if not need:

@@ -152,6 +152,25 @@ def test_binding_refuses_what_the_library_cannot_see():
         dfss.dfss_cache_append(q[0], q[0], None, None, None, None, s)
 
 
+def test_binding_refuses_no_sequences_and_another_devices_workspace():
+    q = torch.zeros(8, 4, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="contiguous"):
+        dfss.dfss_qk_norm_rotate(q, None, None, None, None, Shape(0, 4, 4, 4, 64, 1, 2))
+
+    class Elsewhere:      # (one device here: a tensor's answers, of one that is not the current)
+        is_cuda, device = True, "another"
+        is_contiguous = staticmethod(lambda: True)
+        data_ptr = staticmethod(lambda: 256)
+        get_device = staticmethod(lambda: -1)
+
+    from paper_2203_00091_amd.binding import _scratch
+    assert _scratch(None) is None
+    with pytest.raises(ValueError, match="current device, got one on another"):
+        _scratch(Elsewhere())
+    with pytest.raises(ValueError, match="device tensor"):
+        _scratch(torch.zeros(256, dtype=torch.uint8))
+
+
 # ---- the plain forms themselves ----
 
 

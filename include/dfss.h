@@ -426,7 +426,8 @@ typedef struct {
  * for every row x of Q (weight wq) and of K (weight wk).  wq, wk: device, [d], the shape's dtype, 16-byte
  * aligned; NULL: no norm, z = x.  rotary: NULL for none; its pos is [B, Lq].  K and Ko may both be NULL.
  * Uses B, H (= Q->H), Lq (tokens of a batch element, for queries and keys alike), d (64, 128) and dtype
- * (DFSS_BF16, DFSS_F32) of the shape.  eps: finite and >= 0 (a row of zeros needs eps > 0).
+ * (DFSS_BF16, DFSS_F32) of the shape.  eps: finite and >= 0.  With a weight, mean(x^2) + eps lies between 2^-100 and 2^100, where its
+ * squares and root are normal 32-bit numbers (so a row of zeros needs eps > 0).  At most 2^28 / (heads of Q and K + 4) tokens.
  * Qo, Ko: where the results go; with batch = H*Lq*d, token = d, head = Lq*d that is the [B*H, Lq, d] of the
  * attention calls.  Results may take the place of the inputs (same data and strides); other overlaps are
  * not allowed.  32-bit arithmetic, one rounding at the end. */
@@ -464,7 +465,8 @@ typedef struct {
  * len holds the lengths WITH the new tokens, so that the n tokens of sequence b become its tokens
  * len[b] - n .. len[b] - 1; those whose place would be negative, or Lk or more (a length of at most width * page),
  * are not kept.  Keys are normed with w ([d], bfloat16, 16-byte aligned; NULL: not) and rotated (rotary: NULL for none; its pos is
- * [rows], NULL: the token's place) on the way, in 32 bits, and rounded once.
+ * [rows], NULL: the token's place) on the way, in 64 bits, and rounded once; as in dfss_qk_norm_rotate, the mean of a row's squares
+ * and eps lie between 2^-100 and 2^100 together.
  * The scale of a page and head becomes 2^ceil(log2(amax / 448)), at least 2^-64, over the appended values; where
  * the page holds earlier tokens of the sequence it is at least what it was, and if it grows their codes are
  * rounded again (nearest-even) to the new scale.  Nothing else of the cache is written.  A page that several sequences

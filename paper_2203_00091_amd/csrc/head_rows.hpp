@@ -7,7 +7,8 @@
 
 namespace dfss {
 
-// Eight consecutive elements of a head's row, which one lane holds: 16 bytes of bfloat16, 32 of float.
+// Eight consecutive elements of a head's row, which one lane holds: 16 bytes of bfloat16, 32 of float.  load_once and store_past: what
+// nobody is expected to read again soon goes from the caches first (non-temporal).
 template <typename T>
 struct Eight;
 template <>
@@ -15,6 +16,8 @@ struct Eight<__bf16> {
     u32x4 w;
     __device__ __forceinline__ void load(const __bf16 *p) { w = *reinterpret_cast<const u32x4 *>(p); }
     __device__ __forceinline__ void store(__bf16 *p) const { *reinterpret_cast<u32x4 *>(p) = w; }
+    __device__ __forceinline__ void load_once(const __bf16 *p) { w = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p)); }
+    __device__ __forceinline__ void store_past(__bf16 *p) const { __builtin_nontemporal_store(w, reinterpret_cast<u32x4 *>(p)); }
     __device__ __forceinline__ void get(float *x) const {
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[2 * e] = bf16_lo_to_f32(w[e]), x[2 * e + 1] = bf16_hi_to_f32(w[e]);
@@ -41,6 +44,14 @@ struct Eight<float> {
     __device__ __forceinline__ void store(float *p) const {
         reinterpret_cast<f32x4 *>(p)[0] = a;
         reinterpret_cast<f32x4 *>(p)[1] = b;
+    }
+    __device__ __forceinline__ void load_once(const float *p) {
+        a = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p));
+        b = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(p) + 1);
+    }
+    __device__ __forceinline__ void store_past(float *p) const {
+        __builtin_nontemporal_store(a, reinterpret_cast<f32x4 *>(p));
+        __builtin_nontemporal_store(b, reinterpret_cast<f32x4 *>(p) + 1);
     }
     __device__ __forceinline__ void get(float *x) const {
 #pragma unroll

@@ -11,8 +11,8 @@
 // writes to the attention's layout is 1 KiB in a piece), and it goes through heads, U of them on their way at a time: the angles
 // are read once for all of them.  (A wave that takes the heads of one token instead writes rows of 128 or 256 bytes, each L rows
 // apart: 4 x 2048 tokens of 16 + 4 heads, d = 128, 26.8 us, so 19.7.)
-// Measured: that case, 85 MB, 19.7 us = 4.3 TB/s (a copy of 1 GiB runs at 5.1); gradients, 16 x 512 tokens of 12 + 12 heads, d = 64,
-// float, 151 MB, 31.1 us = 4.9 TB/s and 4.0 for the weights' sums; 4 x 2048 tokens of 16 + 16, d = 128, 202 MB, 44.8 us = 4.5 TB/s and 4.0;
+// Measured: that case, 85 MB, 18.5 us = 4.6 TB/s (a copy of 1 GiB runs at 5.1); gradients, 16 x 512 tokens of 12 + 12 heads, d = 64,
+// float, 151 MB, 31.4 us = 4.8 TB/s and 4.0 for the weights' sums; 4 x 2048 tokens of 16 + 16, d = 128, 202 MB, 42.7 us = 4.7 TB/s and 4.0;
 // eight tokens 4.0 us, which is a launch and two dependent reads.
 #include "dfss_kernels.hpp"
 #include "head_rows.hpp"
@@ -53,8 +53,8 @@ struct Weights {
     }
 };
 
-// A wave: 64 / (d / 8) tokens, and `each` of the heads of Q and then of K.
-template <typename T, int D, int U>
+// A wave: 64 / (d / 8) tokens, and `each` of the heads of Q and then of K.  PAST: results leave the caches first (forward).
+template <typename T, int D, int U, bool PAST>
 __global__ __launch_bounds__(256) void k_norm_rotate(HeadRows Q, HeadRows K, const T *__restrict__ wq, const T *__restrict__ wk,
                                                      float eps, RotaryTable rt, long tokens, int L, HeadRows Qo, HeadRows Ko,
                                                      int parts, int each) {
@@ -99,7 +99,10 @@ __global__ __launch_bounds__(256) void k_norm_rotate(HeadRows Q, HeadRows K, con
                 }
                 turn.apply(a, ao, y);
                 x[u].set(y);
-                if (at.real) x[u].store(at.row<T>(Y, h + u));
+                if (at.real) {
+                    if constexpr (PAST) x[u].store_past(at.row<T>(Y, h + u));
+                    else x[u].store(at.row<T>(Y, h + u));
+                }
             }
         }
     }
@@ -109,6 +112,8 @@ __global__ __launch_bounds__(256) void k_norm_rotate(HeadRows Q, HeadRows K, con
 // which is all that 128 registers let in.  One row in flight in each of these (the two gradient cases above: 31.1 and 44.8 us) is level
 // with two in each of 768 (32.9 and 46.5); two in 1024 do not fit into the registers (42 and 55).
 constexpr int kGradGroups = 1024;
+// The last-level cache.
+constexpr long kCacheBytes = 256L << 20;
 // Waves that the forward pass wants: as many as the chip holds (256 compute units, 32 waves each).
 constexpr long kForwardWaves = 8192;
 
@@ -117,7 +122,8 @@ __device__ __forceinline__ HeadRows either(bool first, const HeadRows &a, const 
 }
 
 // Queries in the first `qgroups` workgroups, keys in the others; a wave goes over units of 64 / (d / 8) tokens and `each` heads.
-template <typename T, int D, int U>
+// PAST: what is read and written leaves the caches first, but for dy (backward).
+template <typename T, int D, int U, bool PAST>
 __global__ __launch_bounds__(256, 4) void k_norm_rotate_grad(HeadRows dQo, HeadRows dKo, HeadRows Q, HeadRows K,
                                                           const T *__restrict__ wq, const T *__restrict__ wk, float eps,
                                                           RotaryTable rt, long tokens, int L, HeadRows dQ, HeadRows dK,
@@ -149,7 +155,11 @@ __global__ __launch_bounds__(256, 4) void k_norm_rotate_grad(HeadRows dQo, HeadR
             for (int u = 0; u < U; ++u)
                 if (h + u < to) {
                     y[u].load(at.row<const T>(Y, h + u));
-                    if (w) x[u].load(at.row<const T>(X, h + u));
+                    if constexpr (PAST) {
+                        if (w) x[u].load_once(at.row<const T>(X, h + u));
+                    } else {
+                        if (w) x[u].load(at.row<const T>(X, h + u));
+                    }
                 }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -177,7 +187,10 @@ __global__ __launch_bounds__(256, 4) void k_norm_rotate_grad(HeadRows dQo, HeadR
                     }
                 }
                 y[u].set(dz);
-                if (at.real) y[u].store(at.row<T>(dX, h + u));
+                if (at.real) {
+                    if constexpr (PAST) y[u].store_past(at.row<T>(dX, h + u));
+                    else y[u].store(at.row<T>(dX, h + u));
+                }
             }
         }
     }
@@ -239,11 +252,18 @@ hipError_t forward(const HeadRows &Q, const HeadRows &K, const void *wq, const v
     const long tokens = B * L, groups = (tokens + TPW - 1) / TPW;
     const int heads = Q.H + K.H, each = heads_each(groups, heads, kForwardWaves), parts = (heads + each - 1) / each;
     const dim3 grid((unsigned)((groups * parts + 3) / 4));
+    // Results of bfloat16 leave the caches first, up to half of the last-level cache: 84 MB (4 x 1024 tokens of 32 + 8 heads, d = 128)
+    // 18.9 us without and 17.6 with it, 100 MB (16 x 1024, 12 + 12, d = 64) 20.5 and 19.2, and behind it 134 MB 24.1 and 24.3, 268 MB 49.5
+    // and 51.4.  Of float a lane stores two halves of 32 bytes, which then leave apart from each other: 100 MB 18.1 and 20.5.
+    const bool past = sizeof(T) == 2 && 2 * tokens * heads * D * (long)sizeof(T) <= kCacheBytes / 2;
 #define DFSS_LAUNCH(U)                                                                                                   \
-    hipLaunchKernelGGL((k_norm_rotate<T, D, U>), grid, dim3(256), 0, st, Q, K, (const T *)wq, (const T *)wk, eps, rt, tokens, L, \
+    if (past) DFSS_PAST(U, sizeof(T) == 2); else DFSS_PAST(U, false)
+#define DFSS_PAST(U, PAST)                                                                                               \
+    hipLaunchKernelGGL((k_norm_rotate<T, D, U, PAST>), grid, dim3(256), 0, st, Q, K, (const T *)wq, (const T *)wk, eps, rt, tokens, L, \
                        Qo, Ko, parts, each)
     // four rows on their way where a wave has four heads to go through; else their registers would only keep waves out
-    if (each >= 4) DFSS_LAUNCH(4); else DFSS_LAUNCH(1);
+    if (each >= 4) { DFSS_LAUNCH(4); } else { DFSS_LAUNCH(1); }
+#undef DFSS_PAST
 #undef DFSS_LAUNCH
     return hipGetLastError();
 }
@@ -263,8 +283,15 @@ hipError_t backward(const HeadRows &dQo, const HeadRows &dKo, const HeadRows &Q,
         if (k && qg > kGradGroups - 1) qg = kGradGroups - 1;
         kg = k ? kGradGroups - qg : 0;
     }
-    hipLaunchKernelGGL((k_norm_rotate_grad<T, D, U>), dim3((unsigned)(qg + kg)), dim3(256), 0, st, dQo, dKo, Q, K, (const T *)wq,
-                       (const T *)wk, eps, rt, tokens, L, dQ, dK, (int)qg, each, part);
+    // A call that leaves little of the last-level cache to others reads x and writes dx past it, so that dy, which was just written, stays:
+    // 202 MB (4 x 2048 tokens of 16 + 16 heads, d = 128) 52.1 us without and 40.6 with it, 403 MB 95.8 and 82.7, float 89.1 and 79.4;
+    // smaller ones find x there, too: 126 MB (4 x 1024, 32 + 8) 31.2 and 34.6, float 151 MB 31.7 and 33.8.
+    const bool past = 3 * tokens * (Q.H + K.H) * D * (long)sizeof(T) > kCacheBytes * 5 / 8;
+#define DFSS_LAUNCH(PAST)                                                                                                \
+    hipLaunchKernelGGL((k_norm_rotate_grad<T, D, U, PAST>), dim3((unsigned)(qg + kg)), dim3(256), 0, st, dQo, dKo, Q, K, (const T *)wq, \
+                       (const T *)wk, eps, rt, tokens, L, dQ, dK, (int)qg, each, part)
+    if (past) DFSS_LAUNCH(true); else DFSS_LAUNCH(false);
+#undef DFSS_LAUNCH
     if (wq || wk)
         hipLaunchKernelGGL((k_norm_weight_grad<D>), dim3(D / 8, 2), dim3(256), 0, st, part, (int)qg, (int)(qg + kg),
                            wq ? dwq : nullptr, wk ? dwk : nullptr);

@@ -214,3 +214,34 @@ def test_many_tokens_and_heads():
         at = torch.tensor([[t]], dtype=torch.int32, device=DEV)
         one, _ = dfss.dfss_qk_norm_rotate(x[b:b + 1, t:t + 1, h:h + 1], None, w, None, Rotary(cos, sin, at), Shape(1, 1, 1, 1, 64, 1, 2))
         assert torch.equal(one[0, 0], whole.view(4, 24, 1500, 64)[b, h, t])
+
+
+def test_calls_that_outgrow_the_last_cache():
+    """What is read and written past the caches, in both directions: the formula without rotation, and with it the same rows in
+    another shape."""
+    B, L, H, Hk, d = 4, 2048, 16, 17, 128
+    g = torch.Generator(device=DEV).manual_seed(20)
+    rnd = lambda *n: torch.randn(n, generator=g, device=DEV).bfloat16()
+    X, dY, w = (rnd(B, L, H, d), rnd(B, L, Hk, d)), (rnd(B, L, H, d), rnd(B, L, Hk, d)), (rnd(d), rnd(d))
+    s = Shape(B, H, L, L, d, 1, 2)
+    got = dfss.dfss_qk_norm_rotate_backward(*dY, *X, *w, None, s, EPS)
+    half = torch.finfo(torch.bfloat16).eps / 2
+    for i in (0, 1):
+        dw, terms = torch.zeros(d, dtype=torch.float64, device=DEV), torch.zeros(d, dtype=torch.float64, device=DEV)
+        for b in range(B):
+            x, dz, f = X[i][b].double(), dY[i][b].double(), w[i].double()
+            r = (x.square().mean(-1, keepdim=True) + EPS).rsqrt()
+            mean = (dz * f * x).mean(-1, keepdim=True)
+            want, amount = r * (dz * f - x * r * r * mean), r * ((dz * f).abs() + (x * r * r).abs() * (dz * f * x).abs().mean(-1, keepdim=True))
+            # one rounding to bfloat16, and at most 32 in 32 bits on the way to each of the amounts
+            assert bool(((got[i][b].double() - want).abs() <= half * want.abs() + 2.01 * 32 * 2.0 ** -24 * amount).all())
+            dw += (dz * x * r).sum((0, 1))
+            terms += (dz * x * r).abs().sum((0, 1))
+        # a term has fewer than 32 roundings, and passes fewer than 128 additions: 8192 x 17 rows over 512 workgroups of 16 rows side by
+        # side are 18, then 2 and 2 in the workgroup and 16 and 5 over all of them
+        assert bool(((got[2 + i].double() - dw).abs() <= 160 * 2.0 ** -24 * terms).all())
+    rotary = Rotary(*(t.to(DEV) for t in _angles(L, d)))
+    whole = dfss.dfss_qk_norm_rotate(*X, *w, rotary, s, EPS)
+    for b in range(B):
+        one = dfss.dfss_qk_norm_rotate(*(x[b:b + 1] for x in X), *w, rotary, Shape(1, H, L, L, d, 1, 2), EPS)
+        assert all(torch.equal(x.view(B, -1, L, d)[b], y) for x, y in zip(whole, one))

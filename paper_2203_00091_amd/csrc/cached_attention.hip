@@ -37,6 +37,12 @@ using namespace cached;
 
 namespace {
 
+template <bool ONCE, typename T>
+__device__ __forceinline__ T load(const T *p) {
+    if constexpr (ONCE) return __builtin_nontemporal_load(p);
+    else return *p;
+}
+
 constexpr float kTau = 8.0f * 1.4426950408889634f;   // how far (in exponents of two) scores may exceed the reference
 // From a block's scores of 16 queries (query l % 16, the lane's 16 keys) to the kept ones' weights as operand of the second
 // product: selection, the reference raised where the block outgrew it (accumulators with it: rows 4 (l / 16) + r), exponentials, row
@@ -87,8 +93,11 @@ __device__ __forceinline__ void weigh(const f32x4 (&s)[4], float c, int kb, bf16
     }
 }
 
+// Codes that are read once (ONCE) leave the caches first: V at d = 128, K at d = 64, whose loads take whole rows (the others take half of
+// one each, and the second half is then no longer there: 64 sequences of up to 4096 keys, 8 key heads, d = 128, 85 us, V 74, K 81 to 86,
+// both 83; 128 of 2048, 16 heads, d = 64, full, 81, V 79, K 74, both 75).
 // BIG: pages of 64 tokens or more, a block lies in one.
-template <int D, int MODE, int NW, int RT, bool BIG>
+template <int D, int MODE, int NW, int RT, bool BIG, bool ONCE>
 __global__ __launch_bounds__(64 * NW, NW == 16 ? 4 : RT == 1 && D == 64 ? 3 : RT <= 2 ? 2 : 1) void k_cached(const __bf16 *__restrict__ Q, const int *__restrict__ cu, PagedCache cache,
                                                     const uint8_t *__restrict__ Kc, const uint8_t *__restrict__ Vc,
                                                     const float *__restrict__ Ks, const float *__restrict__ Vs,
@@ -203,7 +212,7 @@ __global__ __launch_bounds__(64 * NW, NW == 16 ? 4 : RT == 1 && D == 64 ? 3 : RT
             // (DENSE: the last two tiles are those of keys 32 .. 63)
             const uint8_t *const q = Kc + half[t >> 1] + (k_lane + (DENSE ? 4 * (t & 1) + (BIG ? 32 * (t >> 1) : 0) : 4 * t) * D);
 #pragma unroll
-            for (int x = 0; x < SS; ++x) kr[t][x] = *reinterpret_cast<const u32x4 *>(q + 64 * x);
+            for (int x = 0; x < SS; ++x) kr[t][x] = load<ONCE && D == 64>(reinterpret_cast<const u32x4 *>(q + 64 * x));
         }
     };
     auto load_v = [&](const Pages &p, int jb) {
@@ -217,7 +226,7 @@ __global__ __launch_bounds__(64 * NW, NW == 16 ? 4 : RT == 1 && D == 64 ? 3 : RT
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 if constexpr (VW == 2) {
-                    const u32x2 x = *reinterpret_cast<const u32x2 *>(q + e * D);
+                    const u32x2 x = load<ONCE>(reinterpret_cast<const u32x2 *>(q + e * D));
                     vr[st][e][0] = x[0], vr[st][e][VW - 1] = x[1];
                 } else {
                     vr[st][e][0] = *reinterpret_cast<const uint32_t *>(q + e * D);
@@ -523,16 +532,25 @@ hipError_t launch(const HeadRows &Q, int T, const int *cu, int B, int most, int 
 #define DFSS_LAUNCH(KERNEL)                                                                                             \
     hipLaunchKernelGGL((KERNEL), dim3(p.target ? shares : items), dim3(64 * p.NW), 0, st, (const __bf16 *)Q.data, cu, c, c.k, c.v,  \
                        c.k_scale, c.v_scale, c.table, sz, (uint16_t *)O, part)
-#define DFSS_PAGES(NW, RT)                                                                                              \
-    if (c.page_shift >= 6) DFSS_LAUNCH(DFSS_K(NW, RT, true)); else DFSS_LAUNCH(DFSS_K(NW, RT, false))
-#define DFSS_K(NW, RT, BIG) k_cached<D, MODE, NW, RT, BIG>
+#define DFSS_PAGES(NW, RT, ONCE)                                                                                        \
+    if (c.page_shift >= 6) DFSS_LAUNCH(DFSS_K(NW, RT, true, ONCE)); else DFSS_LAUNCH(DFSS_K(NW, RT, false, ONCE))
+#define DFSS_K(NW, RT, BIG, ONCE) k_cached<D, MODE, NW, RT, BIG, ONCE>
+#define DFSS_ROWS(NW, RT)                                                                                               \
+    if (once) { DFSS_PAGES(NW, RT, true); } else { DFSS_PAGES(NW, RT, false); }
+    // Codes leave the caches first where nobody else of the call reads them and they are more than three quarters of the last-level
+    // cache of 256 MB, so far as the host knows: 32 sequences of up to 4096 keys, 8 key heads, four queries, d = 128, 44.3 us and 38.8; 4 of
+    // 32768 keys 48.6 and 45.1; in smaller calls the next one finds them there (16 of 4096 keys, one query, 30.7 and 31.9).
+    const long tokens = (long)B * max_len, room = (long)c.n_pages << c.page_shift;
+    const bool once = p.tiles == 1 && (tokens < room ? tokens : room) * c.Hk * (2 * D) >= 192L << 20;
     if (p.RT == kWide) {
         if (const hipError_t e = launch_wide((const __bf16 *)Q.data, cu, c, D, MODE, sz, p.target ? shares : items, (uint16_t *)O, part, st)) return e;
     } else if (p.RT == 1) {
-        if (p.NW == 16) { if constexpr (D == 64) { DFSS_PAGES(16, 1); } } else if (p.NW == 8) { DFSS_PAGES(8, 1); } else { DFSS_PAGES(4, 1); }
+        // (sixteen waves: 256 workgroups of 80 blocks, 168 MB, at most)
+        if (p.NW == 16) { if constexpr (D == 64) { DFSS_PAGES(16, 1, false); } } else if (p.NW == 8) { DFSS_ROWS(8, 1); } else { DFSS_ROWS(4, 1); }
     } else {
-        if (p.NW == 8) { DFSS_PAGES(8, 2); } else { DFSS_PAGES(4, 2); }
+        if (p.NW == 8) { DFSS_ROWS(8, 2); } else { DFSS_ROWS(4, 2); }
     }
+#undef DFSS_ROWS
 #undef DFSS_K
 #undef DFSS_PAGES
 #undef DFSS_LAUNCH

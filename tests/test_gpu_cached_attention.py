@@ -454,6 +454,30 @@ def test_another_stream():
     assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("mode", MODES, ids=str)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("B, most, queries", [(6, 1 << 23, 1), (6, 1 << 23, 5), (320, 1 << 17, 1), (320, 1 << 17, 5)])
+def test_calls_that_outgrow_the_last_cache(B, most, queries, page, d, mode):
+    """Room for more keys than the last-level cache holds, in a cache of as many pages (most: bytes of K for each sequence and key
+    head); keys shared by workgroups and not."""
+    B = B * 128 // d if B > 6 else B
+    a = Attend(d, page, 2, 4, [((37 * i + 3) % 301, queries) for i in range(B)], 51)
+    max_len = (most if B <= 6 else most * 5 // 4 * d // 128) // d
+    n = -(-(192 << 20) // (2 * 2 * d * page))
+    at = torch.randperm(n, generator=torch.Generator().manual_seed(52))[:a.k.shape[0]].to(DEV)
+    big = []
+    for x in (a.k, a.v):
+        big.append(torch.full((n, 2, page, d), NOTHING, dtype=torch.uint8, device=DEV).index_copy_(0, at, x.to(DEV)))
+    for x in (a.k_scale, a.v_scale):
+        big.append(torch.ones((n, 2), device=DEV).index_copy_(0, at, x.to(DEV)))
+    table = torch.full((B, -(-max_len // page)), -1, dtype=torch.int32, device=DEV)
+    table[:, :a.table.shape[1]] = torch.where(a.table.to(DEV) >= 0, at[a.table.to(DEV).clamp(min=0).long()].int(), -1)
+    assert min(B * max_len, n * page) * 2 * 2 * d >= 192 << 20
+    a.cache = Cache(*big, table, a.cache.len)
+    a.check(a.call(*mode, max_len=max_len), *mode)
+
+
 def test_pages_behind_four_gigabytes():
     """Places in a cache that 32 bits do not hold: the same tokens in the first and in the last pages."""
     page, Hk, d = 128, 8, 128

@@ -13,7 +13,7 @@
 // workgroup.
 //
 // Measured: 8 sequences of up to 2048 tokens (12k in all) x 16 heads, d = 64, pages of 16, 79 MB, 21.6 us = 3.6 TB/s; one token each
-// of 64 sequences, 8 heads, d = 128, pages of 64, 5.8 us: a chain of reads (offsets, length, page, scale, codes of the page if the
+// of 64 sequences, 8 heads, d = 128, pages of 64, 5.4 us: a chain of reads (offsets, length, page, scale, codes of the page if the
 // scale grew), 0.4 MB.
 #include "dfss_kernels.hpp"
 #include "head_rows.hpp"

@@ -19,10 +19,10 @@
 // The keys of a row tile go to the NW waves of a workgroup, and to several workgroups where the tiles are few or the
 // sequences long; partial results (reference, sum, unnormalised O, fp32) are merged in a fixed order.
 //
-// Measured, one query a sequence (bytes of the codes that the lengths reach; a copy of 1 GiB runs at 5.1 TB/s, a sum over it at 4.0):
-//   64 sequences of up to 4096 keys, 32 heads on 8, d = 128, pages of 16, 2:4      404 MB   81 us   5.0 TB/s
-//   128 of up to 2048, 16 heads on 16, d = 64, pages of 32, full                   404 MB   77 us   5.2 TB/s
-//   4 of up to 32768, 32 heads on 8, d = 128, pages of 128, full                   201 MB   42 + 5 (merge) us   4.9 TB/s
+// Measured, one query a sequence (bytes of the codes that the lengths reach; a copy of 1 GiB, half of it writes, runs at 5.1 TB/s):
+//   64 sequences of up to 4096 keys, 32 heads on 8, d = 128, pages of 16, 2:4      404 MB   74 us   5.5 TB/s
+//   128 of up to 2048, 16 heads on 16, d = 64, pages of 32, full                   404 MB   71 us   5.7 TB/s
+//   4 of up to 32768, 32 heads on 8, d = 128, pages of 128, full                   201 MB   40 + 5 (merge) us   5.0 TB/s
 //   24 of up to 2500, four queries, 12 heads on 4, d = 64, pages of 32, 1:2         23 MB   12.4 us: five blocks a wave, one after the other
 //   1 of 4096, 12 heads on 12, d = 64, pages of 64, 2:4                              6 MB   13.2 us: the same, four blocks a wave
 #include <math.h>
@@ -495,7 +495,7 @@ Plan plan(int B, int Hk, int G, int most, int max_len, int d) {
     const int blocks = (max_len + KB - 1) / KB;
     // Eight waves where that is still one workgroup for each compute unit at most: the wave's own chain of blocks sets the time there
     // (4 sequences of 32768 keys, 8 key heads, d = 128, shared: 42 + 5 us, with four waves 48 + 8).  Four where workgroups follow each
-    // other, since a new one then starts sooner (128 sequences of 2048 keys, 16 heads, d = 64: 77, with eight 87).
+    // other, since a new one then starts sooner (128 sequences of 2048 keys, 16 heads, d = 64: 77, with eight 87, both with all codes through the caches).
     p.NW = items <= 256 || p.RT == kWide ? 8 : 4;
     p.target = 0;
     p.least = p.NW;
@@ -510,7 +510,7 @@ Plan plan(int B, int Hk, int G, int most, int max_len, int d) {
     if (items * blocks <= 4096 && p.RT != kWide) p.NW = 4;
     // Workgroups that the chip holds at a time, by their registers and LDS.  Where the sequences alone are that many, sharing only
     // evens their lengths out, which is worth the merge for long ones alone (64 sequences of up to 4096 keys, 8 key heads, d = 128:
-    // 81 us alone, 96 + 6 shared), and with four rounds of them lengths even out by themselves.
+    // 81 us alone, 96 + 6 shared, likewise), and with four rounds of them lengths even out by themselves.
     const long slots = p.NW == 8 ? 256 : 512;
     if (items >= 4 * slots || (items >= slots && blocks < 128)) return p;
     p.least = p.NW;

@@ -893,9 +893,9 @@ def _rows(t: torch.Tensor | None, shape, dtype, what: str, out: bool = False):
     return _ROWS.pack(t.data_ptr(), H, batch, token, head), H
 
 
-def _headed(B: int, H: int, L: int, d: int, dtype, device):
-    """A new [B * H, L, d] and its rows, as _rows gives them."""
-    t = torch.empty((B * H, L, d), dtype=dtype, device=device)
+def _headed(X: torch.Tensor, B: int, H: int, L: int, d: int):
+    """A new [B * H, L, d] of X's type and device, and its rows, as _rows gives them."""
+    t = X.new_empty((B * H, L, d))
     return t, _ROWS.pack(t.data_ptr(), H, H * L * d, d, L * d)
 
 
@@ -910,11 +910,11 @@ def dfss_qk_norm_rotate(Q, K, wq, wk, rotary: Rotary | None, s: Shape, eps: floa
     t, shape = s._call.torch_dtype, (s.B, s.Lq, s.d)
     (q, Hq), (k, Hk) = _rows(Q, shape, t, "Q"), _rows(K, shape, t, "K")
     if Qo is None:
-        Qo, qo = _headed(s.B, Hq, s.Lq, s.d, t, Q.device)
+        Qo, qo = _headed(Q, s.B, Hq, s.Lq, s.d)
     else:
         qo = _rows(Qo, shape, t, "Qo", True)[0]
     if Ko is None and K is not None:
-        Ko, ko = _headed(s.B, Hk, s.Lq, s.d, t, Q.device)
+        Ko, ko = _headed(K, s.B, Hk, s.Lq, s.d)
     else:
         ko = _rows(Ko, shape, t, "Ko", True)[0]
     st = load_library().dfss_qk_norm_rotate(q, k, _weight(wq, t, s.d, "wq"), _weight(wk, t, s.d, "wk"),
@@ -934,9 +934,9 @@ def dfss_qk_norm_rotate_backward(dQo, dKo, Q, K, wq, wk, rotary: Rotary | None, 
     t, shape = s._call.torch_dtype, (s.B, s.Lq, s.d)
     (q, Hq), (k, Hk) = _rows(Q, shape, t, "Q"), _rows(K, shape, t, "K")
     if dQ is None:
-        dQ = torch.empty((s.B, s.Lq, Hq, s.d), dtype=t, device=Q.device)
+        dQ = Q.new_empty((s.B, s.Lq, Hq, s.d))
     if dK is None and K is not None:
-        dK = torch.empty((s.B, s.Lq, Hk, s.d), dtype=t, device=Q.device)
+        dK = K.new_empty((s.B, s.Lq, Hk, s.d))
     if dwq is None and wq is not None:
         dwq = torch.empty(s.d, dtype=torch.float32, device=Q.device)
     if dwk is None and wk is not None and K is not None:
@@ -983,7 +983,7 @@ def _attention_cached(name: str, Q, cu, cache: Cache, s: Shape, scale: float, ca
     n = Q.shape[0]
     (q, H), c = _rows(Q, (n, s.d), torch.bfloat16, "Q"), _cache(cache, s)
     if O is None:
-        O = torch.empty((n, H, s.d), dtype=torch.bfloat16, device=Q.device)
+        O = Q.new_empty((n, H, s.d))
         o = O.data_ptr()
     else:
         o = _array(O, torch.bfloat16, (n, H, s.d), None, "O")

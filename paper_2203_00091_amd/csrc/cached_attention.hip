@@ -484,7 +484,7 @@ __global__ __launch_bounds__(2 * D) void k_cached_merge(const float *__restrict_
 int row_tiles(long rows, int d) { return rows <= 16 ? 1 : rows <= (d == 64 ? 128 : 64) ? 2 : kWide; }
 
 struct Plan {
-    int RT, NW, tiles, target, least;   // NW: waves of a workgroup; target 0: nobody shares
+    int RT, NW, tiles, target, least, fill;   // fill: `per` is the least possible; NW: waves of a workgroup; target 0: nobody shares
 };
 Plan plan(int B, int Hk, int G, int most, int max_len, int d) {
     Plan p;
@@ -499,6 +499,7 @@ Plan plan(int B, int Hk, int G, int most, int max_len, int d) {
     p.NW = items <= 256 || p.RT == kWide ? 8 : 4;
     p.target = 0;
     p.least = p.NW;
+    p.fill = 0;
     // d = 64: sixteen waves walk 80 blocks before a second kernel pays.  12 heads a sequence, 4096 keys, us, sixteen waves, and eight
     // that share the keys with others: 1 sequence 12.7 and 6.1 + 5, 8 of them 14.3 and 13.3 + 5, 20 21.0 and 29.7 + 5; eight waves are
     // enough up to 40 blocks (2000 keys: 9.5 and 9.2).
@@ -518,6 +519,10 @@ Plan plan(int B, int Hk, int G, int most, int max_len, int d) {
     long t = fit > B / 2 ? fit : B / 2 > 0 ? B / 2 : 1;
     const long most_shares = (long)B * ((blocks + p.least - 1) / p.least);
     p.target = (int)(t < most_shares ? t : most_shares);
+    // All shares have a place on the chip at once, and a sequence has four at most: 16 sequences of 6000 keys, 8 key heads, d = 128, 42.5 us
+    // and 37.0 with the least `per`, 8 of 8192, 8 heads, 26.3 and 25.4, 2 of 8192 with 100 queries of 4 heads to a key head 57.9 and 52.2; with
+    // more shares than that the search costs what it gains (7 of 10000, 4 heads, d = 64, 14.9 and 15.5, 4 of 32768 44.8 and 45.0).
+    p.fill = p.target <= fit && B <= 64 && p.target + B <= 4L * B;
     return p;
 }
 // Shares of all sequences, at most (of a valid plan that shares)
@@ -526,7 +531,7 @@ long shares_of(const Plan &p, int B) { return (long)p.target + B; }
 template <int D, int MODE>
 hipError_t launch(const HeadRows &Q, int T, const int *cu, int B, int most, int max_len, float scale, bool causal,
                   const PagedCache &c, void *O, float *part, const Plan &p, hipStream_t st) {
-    const Sizes sz = {T, B, Q.H, Q.H / c.Hk, most, max_len, p.tiles, p.target, p.least, Q.token, Q.head, p.target ? 1. / p.target : 0.,
+    const Sizes sz = {T, B, Q.H, Q.H / c.Hk, most, max_len, p.tiles, p.target, p.least, Q.token, Q.head, p.target ? 1. / p.target : 0., p.fill ? 1. / (p.target + B) : 0.,
                       scale * 1.4426950408889634f, causal ? 1 : 0};
     const unsigned items = (unsigned)((long)B * c.Hk * p.tiles), shares = (unsigned)(shares_of(p, B) * c.Hk * p.tiles);
 #define DFSS_LAUNCH(KERNEL)                                                                                             \

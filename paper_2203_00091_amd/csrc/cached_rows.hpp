@@ -23,14 +23,15 @@ __device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirst
 struct Sizes {
     int T, B, Hq, G, most, max_len, tiles, target, least;   // tiles: row tiles (of 16 RT rows) of a sequence and key head
     long q_token, q_head;
-    double per_target;   // 1 / target
+    double per_target, per_place;   // 1 / target; 1 / (target + B) where `per` is to be the least possible, else 0
     float c;          // scale * log2(e)
     int causal;
 };
 
 // Where keys are shared: sequences are cut into shares of `per` blocks, the same for all of them, so that each of `target`
 // workgroups for every key head and row tile gets about one, whatever the lengths are: per = ceil(all blocks / target), so that all
-// sequences together have at most target + B shares.  They are numbered through the sequences.
+// sequences together have at most target + B shares.  With few shares to a sequence (per_place), the last one of each, which is cut short,
+// leaves much of the chip idle: there `per` is the least that makes no more than target + B shares.  They are numbered through the sequences.
 struct Shares {
     int per;
     // Blocks of a sequence by its length (its row tiles may see fewer under the causal mask).
@@ -58,6 +59,17 @@ struct Shares {
         int p = (int)((double)total * s.per_target);
         p += (long)p * s.target < total;   // rounded up (a division would take ten times the instructions)
         per = scalar(p < s.least ? s.least : p);
+        if (s.per_place == 0.) return;
+        // (a smaller `per` never makes fewer shares, so halving finds it; up to 64 sequences, one to a lane)
+        const int n = l < s.B ? blocks(s, c, l) : 0;
+        int lo = scalar((int)((double)total * s.per_place)), hi = per;
+        lo = lo < s.least ? s.least : lo;
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (__builtin_amdgcn_readlane(scan((n + mid - 1) / mid), 63) <= s.target + s.B) hi = mid;
+            else lo = mid + 1;
+        }
+        per = hi;
     }
     // Number of the first share of sequence `upto`, or (upto < 0) the sequence that share `at` belongs to, and the number of
     // its first one.  Returns -1 if there is no such share.

@@ -276,6 +276,16 @@ def test_long_sequences_are_shared(d, mode):
 
 
 @pytest.mark.parametrize("mode", MODES, ids=str)
+@pytest.mark.parametrize("longest, least", [(6000, 6000), (6000, 1), (6000, 0), (5200, 4000)])
+def test_few_shares_to_a_sequence(longest, least, mode):
+    """Sixteen sequences on a chip that holds 32 shares of them: all alike, most of them empty or of one key, and all but alike."""
+    lengths = [longest if least == longest or b % 5 == 3 else least + 29 * b * (least > 1) for b in range(16)]
+    a = Attend(128, 64, 8, 4, [(n, 1) for n in lengths], 53, uniform=True)
+    assert dfss.dfss_cached_workspace_bytes(a.shape(*mode), a.cache) > 0
+    a.check(a.call(*mode), *mode)
+
+
+@pytest.mark.parametrize("mode", MODES, ids=str)
 def test_rows_that_see_nothing(mode):
     """No tokens, more queries than tokens (the first ones stand before the first key), and pages that are none."""
     a = Attend(64, 16, 1, 2, [(0, 3), (4, 9), (70, 2), (33, 1), (16, 1), (-4, 2)], 37, bad=[(2, 1), (2, 3), (3, 0), (3, 2), (4, 0)])

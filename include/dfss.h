@@ -465,8 +465,8 @@ typedef struct {
  * len holds the lengths WITH the new tokens, so that the n tokens of sequence b become its tokens
  * len[b] - n .. len[b] - 1; those whose place would be negative, or Lk or more (a length of at most width * page),
  * are not kept.  Keys are normed with w ([d], bfloat16, 16-byte aligned; NULL: not) and rotated (rotary: NULL for none; its pos is
- * [rows], NULL: the token's place) on the way, in 64 bits, and rounded once; as in dfss_qk_norm_rotate, the mean of a row's squares
- * and eps lie between 2^-100 and 2^100 together.
+ * [rows], NULL: the token's place) on the way, in 64 bits (the root of the mean to 2^-43), and rounded once, to the nearest code, ties to
+ * even; as in dfss_qk_norm_rotate, the mean of a row's squares and eps lie between 2^-100 and 2^100 together.
  * The scale of a page and head becomes 2^ceil(log2(amax / 448)), at least 2^-64, over the appended values; where
  * the page holds earlier tokens of the sequence it is at least what it was, and if it grows their codes are
  * rounded again (nearest-even) to the new scale.  Nothing else of the cache is written.  A page that several sequences

@@ -12,7 +12,7 @@
 // read and written only if it grew.  A unit is a wave where four of its passes (8 elements in each lane) hold the rows, else a
 // workgroup.
 //
-// Measured: 8 sequences of up to 2048 tokens (12k in all) x 16 heads, d = 64, pages of 16, 79 MB, 21.6 us = 3.6 TB/s; one token each
+// Measured: 8 sequences of up to 2048 tokens (12k in all) x 16 heads, d = 64, pages of 16, 79 MB, 22.6 us = 3.5 TB/s (1 of them to round to odd); one token each
 // of 64 sequences, 8 heads, d = 128, pages of 64, 5.4 us: a chain of reads (offsets, length, page, scale, codes of the page if the
 // scale grew), 0.4 MB.
 #include "dfss_kernels.hpp"
@@ -29,6 +29,15 @@ __device__ __forceinline__ int scale_exponent(float amax) {
     return e < -64 ? -64 : e;
 }
 __device__ __forceinline__ float exp2_int(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }
+
+// y in 32 bits, cut, the lowest bit set where something was cut off (rounded to odd): rounding that to the nearest of fewer bits, or
+// comparing it with a number of fewer, has the outcome that y would have had.
+__device__ __forceinline__ float to_odd(double y) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, y);
+    uint32_t lo = (uint32_t)u;
+    lo = (lo | ((lo & 0x1FFFFFFFu) + 0x1FFFFFFFu)) & 0xE0000000u;
+    return (float)__builtin_bit_cast(double, (u & 0xFFFFFFFF00000000u) | lo);
+}
 
 __device__ __forceinline__ u32x2 encode(const float *x, float inv) {   // eight values, nearest-even
     u32x2 r;
@@ -132,8 +141,9 @@ __global__ __launch_bounds__(256) void k_cache_append(HeadRows K, HeadRows V, in
             turn.load(rt.cos, rt.sin, r < rows ? rt.at(token, start + (token - lo)) : 0, rt.rot, rt.interleaved != 0, l, c, false);
             float xo[8];
             raw[i].of_lane(turn.other).get(xo);
-            // y = r (x w cos + x' w' sin) in 64 bits (x w is exact in 32): a code has a border every 16th of its value, and each 32-bit
-            // rounding on the way would put a few of a million values on the wrong side of theirs.
+            // y = r (x w cos + x' w' sin) in 64 bits (x w is exact in 32) and from there to odd, so that the code is the one rounding: a code
+            // has a border every 16th of its value, and each 32-bit rounding on the way would put some of a million values on the wrong
+            // side of theirs.
             double rn = 1.;
             if (w) {
                 double ss = 0.;
@@ -143,7 +153,7 @@ __global__ __launch_bounds__(256) void k_cache_append(HeadRows K, HeadRows V, in
 #pragma unroll
                 for (int o = LPR / 2; o > 0; o >>= 1) ss += __shfl_xor(ss, o, kWave);
                 ss = ss * (1. / D) + eps;
-                rn = __builtin_amdgcn_rsqf((float)ss);   // 1 / sqrt in 32 bits, and a step of Newton's for 40 and more
+                rn = __builtin_amdgcn_rsqf((float)ss);   // 1 / sqrt to 2^-22, and a step of Newton's: to 2^-43
                 rn = rn * (1.5 - 0.5 * ss * rn * rn);
                 w_mine.get(f);
 #pragma unroll
@@ -156,7 +166,7 @@ __global__ __launch_bounds__(256) void k_cache_append(HeadRows K, HeadRows V, in
             float y[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                y[e] = (float)(rn * __builtin_fma((double)x[i][e], (double)turn.cos[e], (double)(turn.interleaved ? x[i][e ^ 1] : xo[e]) * (double)turn.sin[e]));
+                y[e] = to_odd(rn * __builtin_fma((double)x[i][e], (double)turn.cos[e], (double)(turn.interleaved ? x[i][e ^ 1] : xo[e]) * (double)turn.sin[e]));
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[i][e] = y[e];
         }
@@ -229,7 +239,7 @@ __global__ __launch_bounds__(256) void k_cache_append(HeadRows K, HeadRows V, in
 }
 
 // Waves that fill the chip, at 2 to 4 for each SIMD unit.  The case above has 24k units of a wave: four heads in turn 26.3 us, two 31.1,
-// one 36.2 (21.6 with four since the instances that never need a second pass have none and codes leave the caches first).
+// one 36.2 (22.6 with four since the instances that never need a second pass have none and codes leave the caches first).
 constexpr long kFullWaves = 4096;
 
 }  // namespace

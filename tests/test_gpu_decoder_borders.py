@@ -1,0 +1,43 @@
+"""The calls over a paged cache where a value lies next to a border: of two codes, of two scales, of a choice, of what 32 bits hold."""
+import math
+
+import decoder_reference as ref
+import pytest
+import test_gpu_cached_attention as cached
+import torch
+from test_gpu_cached_attention import DEV, MODES, Append, Attend
+
+import paper_2203_00091_amd as dfss
+from paper_2203_00091_amd import Cache, Rotary, Shape
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- appending ---------------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_key_next_to_the_border_of_two_codes(d, interleaved):
+    """A rotated key 2^-40 above or below the middle of two codes takes the nearer one, though 32 bits would put it on the middle; and
+    one as little above what a scale holds takes the next scale."""
+    ties = [1.0625 + i / 8 for i in range(8)]                       # middles of the codes 1, 1.125 .. 2
+    cos = torch.tensor([ties * 2, [1.75] * 16])                     # [position, pair]
+    sin = torch.full((2, 16), 2.0 ** -40)
+    first, second = (slice(0, 32, 2), slice(1, 32, 2)) if interleaved else (slice(0, 16), slice(16, 32))
+    K = torch.zeros(8, 1, d)
+    for t, (x1, x2, most) in enumerate([(1, 1, 448), (1, -1, 448), (-1, 1, 448), (-1, -1, 448), (256, 256, 1), (256, -256, 1), (256, 0, 1), (-256, -256, 1)]):
+        K[t, 0, first], K[t, 0, second], K[t, 0, d - 1] = x1, x2, most
+    pos = torch.tensor([0] * 4 + [1] * 4)
+    table = torch.arange(8, dtype=torch.int32).flip(0)[:, None].contiguous()      # a page to each token: a scale of its own
+    codes = [torch.zeros(8, 1, 16, d, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    scales = [torch.ones(8, 1, device=DEV) for _ in range(2)]
+    cache = Cache(*codes, *scales, table.to(DEV), torch.ones(8, dtype=torch.int32, device=DEV))
+    rows = K.bfloat16().to(DEV)
+    dfss.dfss_cache_append(rows, rows, None, cache, None, Rotary(cos.to(DEV), sin.to(DEV), pos.int().to(DEV), interleaved), Shape(8, 1, 1, 16, d))
+    exact = ref.norm_rotate(K[None], None, (cos, sin, interleaved), pos[None], 0.0)[0]
+    want = torch.tensor([ref.scale_of(float(exact[t].abs().max())) for t in range(8)])
+    assert want.tolist() == [1, 1, 1, 1, 2, 2, 1, 2]     # 448 and 2^-32 more; (256, 0) turns into 448 and 2^-32
+    assert scales[0].flatten().flip(0).tolist() == want.tolist()
+    got = ref.codes_to_values(codes[0].cpu())[:, 0, 0].flip(0)
+    assert torch.equal(got, ref.nearest(exact[:, 0] / want[:, None]))

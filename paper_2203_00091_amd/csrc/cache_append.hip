@@ -152,7 +152,7 @@ __global__ __launch_bounds__(256) void k_cache_append(HeadRows K, HeadRows V, in
                 for (int e = 0; e < 8; ++e) ss += (double)(x[i][e] * x[i][e]);
 #pragma unroll
                 for (int o = LPR / 2; o > 0; o >>= 1) ss += __shfl_xor(ss, o, kWave);
-                ss = ss * (1. / D) + eps;
+                ss = r < rows ? ss * (1. / D) + eps : 1.;   // (no infinity of a row that is none, where eps is 0)
                 rn = __builtin_amdgcn_rsqf((float)ss);   // 1 / sqrt to 2^-22, and a step of Newton's: to 2^-43
                 rn = rn * (1.5 - 0.5 * ss * rn * rn);
                 w_mine.get(f);

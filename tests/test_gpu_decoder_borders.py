@@ -41,3 +41,11 @@ def test_a_key_next_to_the_border_of_two_codes(d, interleaved):
     assert scales[0].flatten().flip(0).tolist() == want.tolist()
     got = ref.codes_to_values(codes[0].cpu())[:, 0, 0].flip(0)
     assert torch.equal(got, ref.nearest(exact[:, 0] / want[:, None]))
+
+
+def test_no_offset_to_the_mean_of_squares(monkeypatch):
+    """eps = 0 with rows that are not zero: what a wave holds besides them is nobody's."""
+    monkeypatch.setattr(cached, "EPS", 0.0)
+    for d, page in ((64, 16), (128, 64)):
+        a = Append((page, d, 5, [(0, 1), (5, 1), (3, 2), (page - 1, 1), (0, page + 3), (7, 40)], True, d, False), 60)
+        a.check(a.call())

@@ -239,7 +239,7 @@ __global__ __launch_bounds__(64 * NW, NW == 16 ? 4 : RT == 1 && D == 64 ? 3 : RT
     f32x4 acc_o[RT][DT], acc_l[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        m_ref[rt] = -1.0e30f;
+        m_ref[rt] = kNoReference;
         acc_l[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int t = 0; t < DT; ++t) acc_o[rt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -393,7 +393,7 @@ __global__ __launch_bounds__(64 * NW, NW == 16 ? 4 : RT == 1 && D == 64 ? 3 : RT
         for (int r = w; r < 4; r += NW) {
             const int row = 4 * kb + r, at = R.r0 + 16 * rt + row;
             if (at >= R.rows) continue;
-            float m = -1.0e30f;
+            float m = kNoReference;
 #pragma unroll
             for (int g = 0; g < NW; ++g) m = fmaxf(m, slots[g * (NF * 64) + row]);
             float sum = 0.f, o[DT];
@@ -446,7 +446,7 @@ __global__ __launch_bounds__(2 * D) void k_cached_merge(const float *__restrict_
     if (at >= R.rows) return;
     const long step = (long)cache.Hk * sz.tiles * RT * partial_floats<D>();   // from a share to the next one
     const float *P = part + (((long)first * cache.Hk + head) * sz.tiles + tile) * RT * partial_floats<D>() + rt * partial_floats<D>();
-    float m = -1.0e30f, sum = 0.f;
+    float m = kNoReference, sum = 0.f;
     f32x4 a0 = {0.f, 0.f, 0.f, 0.f}, a1 = {0.f, 0.f, 0.f, 0.f};
     for (int s0 = 0; s0 < shares; s0 += AT_ONCE, P += AT_ONCE * step) {
         float ms[AT_ONCE], ls[AT_ONCE], top = m;

@@ -9,6 +9,10 @@ namespace cached {
 constexpr int KB = 64;    // keys per block
 enum { MODE_2TO4 = 0, MODE_1TO2 = 1, MODE_DENSE = 2 };
 
+// The softmax reference (in raw scores) of a query that has seen no key yet: below all that the calls allow (scaled scores to 2^24 under
+// a scale of 2^-100: 2^124 = 2.1e37) by so much that the first one seen replaces it (7.9e37 x 2^-100 is 6e7).
+constexpr float kNoReference = -1.0e38f;
+
 // A load at an address that is the same in every lane, of memory that no kernel of the call writes, by the scalar unit: what
 // follows from it (pages, addresses) stays off the vector unit.
 template <typename T>

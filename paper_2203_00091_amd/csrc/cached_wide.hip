@@ -354,7 +354,7 @@ __global__ __launch_bounds__(512, 2) void k_cached_wide(const __bf16 *__restrict
         if (team == 0) next();
         bad = bad_after;
     }
-    float m_ref = unset ? -1.0e30f : cref;
+    float m_ref = unset ? kNoReference : cref;
 
     // The second team's results join the first one's: value f of lane l of wave w at float w NF 64 + f 64 + l.
     __syncthreads();

@@ -1,6 +1,4 @@
 """The calls over a paged cache where a value lies next to a border: of two codes, of two scales, of a choice, of what 32 bits hold."""
-import math
-
 import decoder_reference as ref
 import pytest
 import test_gpu_cached_attention as cached
@@ -49,3 +47,37 @@ def test_no_offset_to_the_mean_of_squares(monkeypatch):
     for d, page in ((64, 16), (128, 64)):
         a = Append((page, d, 5, [(0, 1), (5, 1), (3, 2), (page - 1, 1), (0, page + 3), (7, 40)], True, d, False), 60)
         a.check(a.call())
+
+
+# ---- attention ---------------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("mode", MODES, ids=str)
+@pytest.mark.parametrize("sign", [-1, 1])
+@pytest.mark.parametrize("scale", [2.0 ** -90, 2.0 ** -100])
+@pytest.mark.parametrize("lengths, queries", [([1, 40, 130, 300, 9000], 1), ([1, 40, 130, 300, 9000], 20), ([1, 40, 130, 300, 6000], 150)])
+def test_large_scores_under_a_small_scale(lengths, queries, scale, sign, mode):
+    """Scaled scores beyond 2^22 (raw ones to 2^122), all below 0 or all above it.  One key is 64 above the others, so O is its value: the
+    others weigh e^-64."""
+    for d, page in ((64, 64), (128, 16)):
+        a = Attend(d, page, 1, 2, [(n, 1) for n in lengths], 63)
+        counts = [min(n, queries) for n in lengths]
+        a.counts, a.max_q = counts, max(counts)
+        a.cu = torch.tensor([0] + counts).cumsum(0).int().to(DEV)
+        # q . k = 2^22 (sign + j 2^-22) / scale with j = -64, or 0 for the best key: both parts, and their sum, are 32-bit numbers
+        Q = torch.zeros(sum(counts), 2, d)
+        Q[..., 0], Q[..., 1] = sign * 2.0 ** 10 / scale, -1 / scale * 2.0 ** -12
+        K = torch.zeros(a.k.shape[0], 1, page, d)
+        K[..., 0], K[..., 1] = 2.0 ** 12, 64 * 2.0 ** 12
+        best = [(n - 1) // 3 if i % 2 else 0 for i, n in enumerate(lengths)]
+        for b, j in enumerate(best):
+            K[int(a.table[b, j // page]), 0, j % page, 1] = 0
+        a.k, a.k_scale = (K / 2.0 ** 12).to(torch.float8_e4m3fn).view(torch.uint8), torch.full(a.k_scale.shape, 2.0 ** 12)
+        a.Q, a.scale = Q.bfloat16().to(DEV), scale
+        a.cache = Cache(*(x.to(DEV) for x in (a.k, a.v, a.k_scale, a.v_scale)), a.table.to(DEV), a.cache.len)
+        O, at = a.call(*mode, causal=False).cpu().double(), 0
+        for b, (n, j) in enumerate(zip(counts, best)):
+            id = int(a.table[b, j // page])
+            v = ref.codes_to_values(a.v[id, 0, j % page]) * float(a.v_scale[id, 0])
+            assert torch.equal(O[at:at + n], v.expand(n, 2, d)), (d, b)
+            at += n

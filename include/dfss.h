@@ -482,7 +482,7 @@ dfss_status dfss_cache_append(const dfss_rows *K, const dfss_rows *V, int32_t ro
  * multiple of Hk: heads h*G .. h*G + G - 1 read key head h, G = H / Hk.  cu as above.  Lq: the most queries of a
  * sequence, Lk: the most keys; queries from Lq on are not computed, keys from Lk on not seen.  With causal != 0 the n queries of
  * sequence b are its last n tokens: query i sees keys 0 .. len[b] - n + i; otherwise all len[b].  A query that
- * sees no key gets 0.  Selection as everywhere: larger score wins, equal scores -> lower key; hidden keys lose to all others and weigh 0.
+ * sees no key gets 0.  Selection: of the 32-bit scores q . k the larger wins, equal ones -> lower key; hidden keys lose to all others and weigh 0.
  * scale: 2^-100 to 2^100; scaled scores stay below 2^24 in magnitude (beyond it 32 bits do not tell them apart).
  * O: device, bfloat16 [rows, H, d], 16-byte aligned; rows of no sequence are not written.
  * ws: device, 256-byte aligned, dfss_cached_workspace_bytes(s, cache) bytes (may be 0, then it may be NULL), contents

@@ -7,11 +7,14 @@
 // SIMD unit, without partial results in memory (two workgroups that share the keys: 111 us, and 12 for the merge).  The next
 // block's codes are in registers while this one is worked on, those after it on their way; one barrier a block.
 //
-// Scores, selection and products are those of k_fused32 (fused_attention32.hip): 32 x 32 tiles, scores relative to the softmax
-// reference c from the accumulator on, the position of a score in its two lowest bits.  Hidden keys have the score -3e38; a query that has
-// seen no key yet has no reference (c = 0, and nothing it adds up counts).
-// With 16 x 16 tiles and exact comparisons 97 us, so 82 (of 22 at the rate of a large matrix product).  What bounds it then is the rate at which two waves of a SIMD unit issue: about 540
-// instructions a block and wave.  (Level: the tiles of the first product in turn, more operands ahead, the teams in step.)
+// Tiles and products are those of k_fused32 (fused_attention32.hip): 32 x 32.  Scores and selection are those of k_cached: whole 32-bit
+// scores are compared, and the reference comes in behind that, so a query keeps the same keys whatever else is in the call (but for
+// the order of a 32-bit sum).  (With scores relative to the reference from the accumulator on and the position in the two lowest bits, as
+// k_fused32 has it, small scores are lost at the reference's magnitude, and it is no faster here: 4 x 512 queries of 16 heads on 4, up to 4096 keys, d = 128, 2:4 75.8 us, so
+// 71.1; 1:2 74.5 and 68.3; full 78.0 and 71.7; d = 64 56.6 and 54.1, 55.3 and 47.1, 59.8 and 50.1; d = 128, 2:4, pages of 16 78.9 and
+// 78.7.)
+// What bounds it is the rate at which two waves of a SIMD unit issue: about 450 instructions a block and wave.  (Level: the tiles
+// of the first product in turn, more operands ahead, the teams in step.)
 #include <math.h>
 
 #include "cached_rows.hpp"
@@ -24,18 +27,7 @@ namespace {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-// Distance of the reference above the row maximum that it was set from, in scaled scores; in raw ones at most kMostTau, whatever the
-// scale: scores are rounded at the magnitude of s' = q . k - c, and the comparison has to tell raw scores apart.
-constexpr float kTau = 4.0f, kMostTau = 64.0f;
-constexpr float kHidden = -3.0e38f;
-
-__device__ __forceinline__ float with_position(float v, uint32_t pos) {
-    return __uint_as_float((__float_as_uint(v) & 0xFFFFFFFCu) | pos);
-}
-// idx = (idx >> 2) | (low two bits of v) << 30: sixteen of these fill idx with sixteen positions, first one lowest
-__device__ __forceinline__ uint32_t push_position(uint32_t idx, float v) {
-    return __builtin_amdgcn_alignbit(__float_as_uint(v), idx, 2);
-}
+constexpr float kTau = 8.0f * 1.4426950408889634f;   // how far (in exponents of two) scores may exceed the reference
 
 // BIG: pages of 64 tokens or more, a block lies in one.
 template <int D, int MODE, bool BIG>
@@ -179,19 +171,12 @@ __global__ __launch_bounds__(512, 2) void k_cached_wide(const __bf16 *__restrict
             }
         }
     };
-    const float k2 = sz.c;                                   // weight = exp2(s' k2)
-    const float tau = fminf(kTau * 1.4426950408889634f / sz.c, kMostTau);   // in units of the raw dot product
-    // References are multiples of a power of two: of 1, so that scores of whole numbers stay exact, or less where a whole number is much
-    // to a scaled score (a reference far above the scores would leave weights of 0 only).
-    int above = (int)(__float_as_uint(sz.c) >> 23) - 126;
-    above = above < 100 ? above : 100;
-    const float unit = __uint_as_float((uint32_t)(above > 0 ? 127 - above : 127) << 23), per_unit = __uint_as_float((uint32_t)(above > 0 ? 127 + above : 127) << 23);
-    float cref = 0.f;                                        // reference of query lj (raw dot product)
-    bool unset = true;                                       // it has none yet
-    f32x16 cneg, acc_o[DT], acc_l;                           // -cref, from which the score tiles start
+    const float k2 = sz.c;                                   // weight = exp2((s - reference) k2)
+    float m_ref = kNoReference;                              // reference of query lj (raw dot product)
+    f32x16 acc_o[DT], acc_l;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-        cneg[r] = acc_l[r] = 0.f;
+        acc_l[r] = 0.f;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) acc_o[dt][r] = 0.f;
     }
@@ -233,7 +218,8 @@ __global__ __launch_bounds__(512, 2) void k_cached_wide(const __bf16 *__restrict
         if (jb < end && jb * KB < seen) {   // (the same in every lane)
             const u32x4 *const kt = lds[buf][0];
             const char *const vt = reinterpret_cast<const char *>(lds[buf][1]);
-            // acc[t][4 g + x] = q . k - cref for query lj, key 64 jb + 32 t + 16 h + 4 g + x
+            // acc[t][4 g + x] = q . k for query lj, key 64 jb + 32 t + 16 h + 4 g + x
+            constexpr f32x16 zero = {};
             f32x16 acc[2];
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -241,7 +227,7 @@ __global__ __launch_bounds__(512, 2) void k_cached_wide(const __bf16 *__restrict
                 for (int s = 0; s < STEPS; ++s) {
                     const int slot = 32 * t + lj;
                     const bf16x8 a = __builtin_bit_cast(bf16x8, kt[slot * CPR + ((2 * s + h) ^ operand_row_swizzle<CPR, 32>(slot))]);
-                    acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, bq[s], s == 0 ? cneg : acc[t], 0, 0, 0);
+                    acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, bq[s], s == 0 ? zero : acc[t], 0, 0, 0);
                 }
             read_ahead<2 * STEPS, 1, 2, 1>();
             if (jb * KB + KB > seen_by_all || bad) {
@@ -251,53 +237,34 @@ __global__ __launch_bounds__(512, 2) void k_cached_wide(const __bf16 *__restrict
                     const bool none = bad >> (2 * t + h) & 1;
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
-                        if (32 * t + r >= left || none) acc[t][r] = kHidden;
+                        if (32 * t + r >= left || none) acc[t][r] = -INFINITY;
                 }
             }
-            float kept[2][2 * NP];
+            float kept[2][2 * NP], m_blk = -3.0e38f;
             uint32_t idx = 0;       // positions: tile 0 in the low half
-            for (int pass = 0; pass < 3; ++pass) {   // (two do; with scores that are no numbers, as many as this)
-                float m_blk = -3.0e38f;
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        const float a0 = acc[t][4 * g], a1 = acc[t][4 * g + 1], a2 = acc[t][4 * g + 2], a3 = acc[t][4 * g + 3];
-                        if constexpr (MODE == MODE_2TO4) {
-                            const float e0 = with_position(a0, 0), e1 = with_position(a1, 1), e2 = with_position(a2, 2), e3 = with_position(a3, 3);
-                            const float hi3 = fmaxf(fmaxf(e0, e1), e2), md3 = __builtin_amdgcn_fmed3f(e0, e1, e2);
-                            kept[t][2 * g] = fmaxf(hi3, e3);                                // largest of the four
-                            kept[t][2 * g + 1] = __builtin_amdgcn_fmed3f(hi3, md3, e3);     // second largest
-                            idx = push_position(push_position(idx, kept[t][2 * g]), kept[t][2 * g + 1]);
-                            m_blk = fmaxf(m_blk, kept[t][2 * g]);
-                        } else if constexpr (MODE == MODE_1TO2) {
-                            kept[t][2 * g] = fmaxf(with_position(a0, 0), with_position(a1, 1));     // larger of each pair
-                            kept[t][2 * g + 1] = fmaxf(with_position(a2, 2), with_position(a3, 3));
-                            idx = push_position(push_position(idx, kept[t][2 * g]), kept[t][2 * g + 1]);
-                            m_blk = fmaxf(fmaxf(m_blk, kept[t][2 * g]), kept[t][2 * g + 1]);
-                        } else {
-                            kept[t][4 * g] = a0, kept[t][4 * g + 1] = a1, kept[t][4 * g + 2] = a2, kept[t][4 * g + 3] = a3;
-                            m_blk = fmaxf(m_blk, fmaxf(fmaxf(a0, a1), fmaxf(a2, a3)));
-                        }
+                for (int g = 0; g < 4; ++g) {
+                    const float a0 = acc[t][4 * g], a1 = acc[t][4 * g + 1], a2 = acc[t][4 * g + 2], a3 = acc[t][4 * g + 3];
+                    if constexpr (DENSE) {
+                        kept[t][4 * g] = a0, kept[t][4 * g + 1] = a1, kept[t][4 * g + 2] = a2, kept[t][4 * g + 3] = a3;
+                        m_blk = fmaxf(m_blk, fmaxf(fmaxf(a0, a1), fmaxf(a2, a3)));
+                    } else {
+                        float &lo = kept[t][2 * g], &hi = kept[t][2 * g + 1];
+                        uint32_t code;
+                        if constexpr (MODE == MODE_2TO4) select_2of4(a0, a1, a2, a3, 16 * t + 4 * g, lo, hi, code);
+                        else select_1of2(a0, a1, a2, a3, 16 * t + 4 * g, lo, hi, code);
+                        idx |= code;
+                        m_blk = fmaxf(fmaxf(m_blk, lo), hi);
                     }
-                // a first score, or one at or above the reference (not negative): set the reference, redo the block
-                const float least = unset ? 0.5f * kHidden : 0.f;
-                if (!__any(m_blk >= least)) break;
-                const float mq = fmaxf(m_blk, __shfl_xor(m_blk, 32, 64));   // lanes lj and lj + 32 hold different keys of the same query
-                const bool up = mq >= least;
-                // (above the row maximum by more than its rounding: after this pass every score of the block is negative)
-                const float most = cref + mq + tau;
-                const float c_new = up ? (__builtin_ceilf((most + 0x1p-22f * __builtin_fabsf(most)) * per_unit) + 1.f) * unit : cref;
-                const float delta = c_new - cref;
-                const float alpha = up && !unset ? __builtin_amdgcn_exp2f(-delta * k2) : 1.f;
-                cref = c_new;
-                unset = unset && !up;
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    cneg[r] = -cref;
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) acc[t][r] -= delta;
                 }
+            if constexpr (!DENSE) arrived(idx);   // (formed here: its lane masks are more than there are scalar registers for behind the branch)
+            if (__any((m_blk - m_ref) * k2 > kTau)) {
+                m_blk = fmaxf(m_blk, __shfl_xor(m_blk, 32, 64));   // lanes lj and lj + 32 hold different keys of the same query
+                const float m_new = (m_blk - m_ref) * k2 > kTau ? m_blk : m_ref;
+                const float alpha = __builtin_amdgcn_exp2f((m_ref - m_new) * k2);
+                m_ref = m_new;
                 // accumulator rows are queries 8 (r/4) + 4 h + r%4: their factors from those columns' lanes
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
@@ -306,14 +273,15 @@ __global__ __launch_bounds__(512, 2) void k_cached_wide(const __bf16 *__restrict
 #pragma unroll
                     for (int dt = 0; dt < DT; ++dt) acc_o[dt][r] *= a_r;
                 }
-                idx = 0;
             }
+            const float mb = fmaxf(m_ref * k2, -1.0e37f);   // (no infinity while there is no reference: -inf + inf is no weight)
             uint32_t pk[2][NP];
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int e = 0; e < NP; ++e)
-                    pk[t][e] = pack_bf16x2(__builtin_amdgcn_exp2f(kept[t][2 * e] * k2), __builtin_amdgcn_exp2f(kept[t][2 * e + 1] * k2));
+                    pk[t][e] = pack_bf16x2(__builtin_amdgcn_exp2f(__builtin_fmaf(kept[t][2 * e], k2, -mb)),
+                                           __builtin_amdgcn_exp2f(__builtin_fmaf(kept[t][2 * e + 1], k2, -mb)));
             auto tr = [&](int key0, int dt) {
                 const int chunk = (4 * dt + 2 * tr_colgrp + tr_sub) ^ tr_xor;
                 return lds_read_tr16(vt + ((key0 + tr_row) * CPR + chunk) * 16 + tr_byte);
@@ -354,7 +322,6 @@ __global__ __launch_bounds__(512, 2) void k_cached_wide(const __bf16 *__restrict
         if (team == 0) next();
         bad = bad_after;
     }
-    float m_ref = unset ? kNoReference : cref;
 
     // The second team's results join the first one's: value f of lane l of wave w at float w NF 64 + f 64 + l.
     __syncthreads();

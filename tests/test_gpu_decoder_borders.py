@@ -81,3 +81,22 @@ def test_large_scores_under_a_small_scale(lengths, queries, scale, sign, mode):
             v = ref.codes_to_values(a.v[id, 0, j % page]) * float(a.v_scale[id, 0])
             assert torch.equal(O[at:at + n], v.expand(n, 2, d)), (d, b)
             at += n
+
+
+@pytest.mark.parametrize("mode", MODES, ids=str)
+@pytest.mark.parametrize("size", [2.0 ** -10, 2.0 ** -16, 2.0 ** -30])
+@pytest.mark.parametrize("queries", [1, 20, 150])
+def test_small_scores_are_told_apart(queries, size, mode):
+    """The larger score wins by however little, in calls of few rows and of many: exact scores with ties, and any."""
+    for d, page in ((64, 64), (128, 16)):
+        a = Attend(d, page, 1, 4, [(300, queries), (130, min(queries, 130))], 61, integers=True)
+        a.Q = a.Q * size
+        a.check(a.call(*mode), *mode, all_rows=True)
+        b = Attend(d, page, 2, 2, [(300, queries), (130, min(queries, 130))], 62, size=size)
+        want, amount, gap = b.reference(*mode)
+        # 32 bits: d products, each rounded once on its way into the sum, of |q| |k| altogether (|k| <= 448 x 2^-5)
+        clear = gap > d * 2.0 ** -24 * 14 * b.Q.cpu().double().abs().sum(-1)
+        assert float(clear.double().mean()) > 0.5
+        half = torch.finfo(torch.bfloat16).eps / 2          # (as in Attend.check)
+        tol = half * want.abs() + (half + 1e-5) * (amount + want.abs()) * 1.01
+        assert float(((b.call(*mode).cpu().double() - want).abs() - tol)[clear].max()) <= 0

@@ -40,7 +40,7 @@ EXPORTS = (
     "dfss_cache_append", "dfss_cached_workspace_bytes", "dfss_attention_cached", "dense_attention_cached",
 )
 # exported for the library's own tests only (csrc/dfss_internal.h)
-INTERNAL_EXPORTS = ("dfss_internal_attention_variant",)
+INTERNAL_EXPORTS = ("dfss_internal_attention_variant", "dfss_internal_norm_plan", "dfss_internal_append_plan", "dfss_internal_cached_plan")
 VARIANT_AUTO, VARIANT_Q16, VARIANT_Q16X2, VARIANT_Q32W2, VARIANT_Q32W4, VARIANT_Q32K2, VARIANT_FEW = range(7)
 
 
@@ -773,6 +773,15 @@ def dfss_meta_from_canonical(canon, s: Shape, meta=None):
     st = load_library().dfss_meta_from_canonical(_meta(canon, s), s._call.ref, _meta(meta, s), _stream())
     _check("dfss_meta_from_canonical", st)
     return meta
+
+
+def internal_plan(call: str, *sizes: int):
+    """Which instances a decoder's call ("norm", "append", "cached") runs (tests only; csrc/dfss_internal.h): whole numbers."""
+    out = (ctypes.c_int32 * (4 if call == "cached" else 3))()
+    f = getattr(load_library(), f"dfss_internal_{call}_plan")
+    f.restype = None
+    f(*(ctypes.c_int32(x) for x in sizes), out)
+    return tuple(out)
 
 
 # ---- around a decoder's attention ------------------------------------------------------------------------------

@@ -870,6 +870,22 @@ dfss_status dense_attention_cached(const dfss_rows *Q, int32_t rows, const int32
     return attention_cached(Q, rows, cu, cache, s, true, scale, causal, O, ws, ws_bytes, stream);
 }
 
+// Test hooks (csrc/dfss_internal.h).
+void dfss_internal_norm_plan(int32_t tokens, int32_t heads, int32_t d, int32_t elem, int32_t out[3]) {
+    const dfss::NormPlan p = dfss::norm_rotate_plan(tokens, heads, d, elem);
+    out[0] = p.heads, out[1] = p.past, out[2] = p.past_grad;
+}
+
+void dfss_internal_append_plan(int32_t rows, int32_t ragged, int32_t B, int32_t most, int32_t page, int32_t Hk, int32_t d, int32_t out[3]) {
+    const dfss::AppendPlan p = dfss::append_plan(rows, ragged != 0, B, most, page, Hk, d);
+    out[0] = p.wave ? 1 : 4, out[1] = p.passes, out[2] = p.each;
+}
+
+void dfss_internal_cached_plan(int32_t B, int32_t Hq, int32_t Hk, int32_t most, int32_t max_len, int32_t d, int32_t out[4]) {
+    const dfss::CachedPlan p = dfss::cached_plan(B, Hq, Hk, most, max_len, d);
+    out[0] = p.row_tiles, out[1] = p.waves, out[2] = p.target > 0, out[3] = p.fill;
+}
+
 const char *dfss_status_string(dfss_status st) {
     switch (st) {
         case DFSS_OK: return "ok";

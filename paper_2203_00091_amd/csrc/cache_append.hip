@@ -244,20 +244,27 @@ constexpr long kFullWaves = 4096;
 
 }  // namespace
 
-hipError_t launch_cache_append(const HeadRows &K, const HeadRows &V, int T, const int *cu, int B, int most, int max_len, int d,
-                               const void *w, float eps, const RotaryTable &rt, const PagedCache &c, hipStream_t st) {
-    const int page = 1 << c.page_shift;
-    const unsigned slots = cu ? (unsigned)(T / page + 2 * B) : (unsigned)B * (unsigned)((most - 1) / page + 2);
+AppendPlan append_plan(int T, bool ragged, int B, int most, int page, int Hk, int d) {
+    AppendPlan p;
+    p.slots = ragged ? (unsigned)(T / page + 2 * B) : (unsigned)B * (unsigned)((most - 1) / page + 2);
     // Rows that a call adds to a page, at most -- or, where the calls are those of a step of generation (about a token for each
     // sequence), most likely.  As few registers as those rows need: of many short units waves wait for memory one after the other.
-    const int added = cu ? (T <= 2 * B ? 2 : T) : most, rows = page < added ? page : added, passes = (rows * (d / 8) + 63) / 64;
-    const bool wave = passes <= 4;
+    const int added = ragged ? (T <= 2 * B ? 2 : T) : most, rows = page < added ? page : added;
+    p.passes = (rows * (d / 8) + 63) / 64;
+    p.wave = p.passes <= 4;
     // heads that a unit takes one after the other, its next rows on their way: as many as leave the chip full
-    const long waves = (long)slots * 2 * c.Hk * (wave ? 1 : 4);
-    const int each = waves >= 4 * kFullWaves ? 4 : waves >= 2 * kFullWaves ? 2 : 1, heads = each * (wave ? 4 : 1);
-    const dim3 grid(slots, 2 * (unsigned)((c.Hk + heads - 1) / heads));
+    const long waves = (long)p.slots * 2 * Hk * (p.wave ? 1 : 4);
+    p.each = waves >= 4 * kFullWaves ? 4 : waves >= 2 * kFullWaves ? 2 : 1;
+    return p;
+}
+
+hipError_t launch_cache_append(const HeadRows &K, const HeadRows &V, int T, const int *cu, int B, int most, int max_len, int d,
+                               const void *w, float eps, const RotaryTable &rt, const PagedCache &c, hipStream_t st) {
+    const AppendPlan p = append_plan(T, cu != nullptr, B, most, 1 << c.page_shift, c.Hk, d);
+    const int passes = p.passes, heads = p.each * (p.wave ? 4 : 1);
+    const dim3 grid(p.slots, 2 * (unsigned)((c.Hk + heads - 1) / heads));
 #define DFSS_LAUNCH(D, WU, NP)                                                                                          \
-    hipLaunchKernelGGL((k_cache_append<D, WU, NP>), grid, dim3(256), 0, st, K, V, T, cu, B, most, max_len, (const __bf16 *)w, eps, rt, c, each)
+    hipLaunchKernelGGL((k_cache_append<D, WU, NP>), grid, dim3(256), 0, st, K, V, T, cu, B, most, max_len, (const __bf16 *)w, eps, rt, c, p.each)
     // 12k tokens x 1024 elements, us: one wave of eight passes 30.5 (d = 128, pages of 32) and 31.6 (64, 64), four of two 27.4 and
     // 27.5; four waves of eight 33.5 (128, 64), of four 28.8.
 #define DFSS_PASSES(D)                                                                                                  \

@@ -566,6 +566,11 @@ hipError_t launch(const HeadRows &Q, int T, const int *cu, int B, int most, int 
 
 }  // namespace
 
+CachedPlan cached_plan(int B, int Hq, int Hk, int most, int max_len, int d) {
+    const Plan p = plan(B, Hk, Hq / Hk, most, max_len, d);
+    return CachedPlan{p.RT, p.NW, p.target, p.fill};
+}
+
 size_t cached_workspace_bytes(int B, int Hq, int Hk, int most, int max_len, int d) {
     const Plan p = plan(B, Hk, Hq / Hk, most, max_len, d);
     return p.target ? (size_t)shares_of(p, B) * Hk * p.tiles * p.RT * 16 * (d + 2) * sizeof(float) : 0;

@@ -32,6 +32,14 @@ dfss_status dfss_internal_attention_variant(const void *Q, const void *K, const 
                                             const dfss_shape *s, float scale, void *O, int variant, int dense,
                                             void *stream);
 
+/* Which instances the calls around a decoder's attention run, of sizes that they accept (nothing is launched).
+ *   norm:   tokens, heads of Q and K, d, bytes of an element -> heads in flight; results past the caches: forward, backward
+ *   append: rows, offsets given or not, sequences, tokens each (without offsets), page, Hk, d -> waves of a unit, its passes, its heads
+ *   cached: sequences, Hq, Hk, most queries, most keys, d -> 16-row tiles and waves of a workgroup; keys are shared; with the least shares */
+void dfss_internal_norm_plan(int32_t tokens, int32_t heads, int32_t d, int32_t elem, int32_t out[3]);
+void dfss_internal_append_plan(int32_t rows, int32_t ragged, int32_t B, int32_t most, int32_t page, int32_t Hk, int32_t d, int32_t out[3]);
+void dfss_internal_cached_plan(int32_t B, int32_t Hq, int32_t Hk, int32_t most, int32_t max_len, int32_t d, int32_t out[4]);
+
 #ifdef __cplusplus
 }
 #endif

@@ -166,6 +166,13 @@ hipError_t launch_norm_rotate_grad(const HeadRows &dQo, const HeadRows &dKo, con
 // New tokens (rows of K and V, cu[b] .. cu[b + 1] - 1 for sequence b, or `most` each without cu) into the cache.
 hipError_t launch_cache_append(const HeadRows &K, const HeadRows &V, int T, const int *cu, int B, int most, int max_len, int d,
                                const void *w, float eps, const RotaryTable &rt, const PagedCache &c, hipStream_t st);
+// What a call runs, by its sizes alone (for the launches and the test hooks).
+struct NormPlan { int heads; bool past, past_grad; };     // heads in flight (1, 4); results past the caches, forward and backward
+NormPlan norm_rotate_plan(long tokens, int heads, int d, int elem);
+struct AppendPlan { unsigned slots; int passes, each; bool wave; };   // passes of a unit, heads one after the other; a unit is a wave, or four
+AppendPlan append_plan(int T, bool ragged, int B, int most, int page, int Hk, int d);
+struct CachedPlan { int row_tiles, waves, target, fill; };   // 16-row tiles and waves of a workgroup; target 0: nobody shares keys
+CachedPlan cached_plan(int B, int Hq, int Hk, int most, int max_len, int d);
 // Attention over the cache.  mode: 0 = 2:4, 1 = 1:2, 2 = dense; part: cached_workspace_bytes (may be 0).
 size_t cached_workspace_bytes(int B, int Hq, int Hk, int most, int max_len, int d);
 hipError_t launch_attention_cached(const HeadRows &Q, int T, const int *cu, int B, int most, int max_len, int d, int mode,

@@ -245,17 +245,24 @@ int heads_each(long groups, int heads, long waves) {
     return (int)((heads + parts - 1) / parts);
 }
 
+// Results of bfloat16 leave the caches first, up to half of the last-level cache: 84 MB (4 x 1024 tokens of 32 + 8 heads, d = 128)
+// 18.9 us without and 17.6 with it, 100 MB (16 x 1024, 12 + 12, d = 64) 20.5 and 19.2, and behind it 134 MB 24.1 and 24.3, 268 MB 49.5
+// and 51.4.  Of float a lane stores two halves of 32 bytes, which then leave apart from each other: 100 MB 18.1 and 20.5.
+bool forward_past(long tokens, int heads, int d, int elem) { return elem == 2 && 2 * tokens * heads * d * elem <= kCacheBytes / 2; }
+// A call that leaves little of the last-level cache to others reads x and writes dx past it, so that dy, which was just written, stays:
+// 202 MB (4 x 2048 tokens of 16 + 16 heads, d = 128) 52.1 us without and 40.6 with it, 403 MB 95.8 and 82.7, float 89.1 and 79.4;
+// smaller ones find x there, too: 126 MB (4 x 1024, 32 + 8) 31.2 and 34.6, float 151 MB 31.7 and 33.8.
+bool backward_past(long tokens, int heads, int d, int elem) { return 3 * tokens * heads * d * elem > kCacheBytes * 5 / 8; }
+int forward_each(long tokens, int heads, int d) { return heads_each((tokens + 512 / d - 1) / (512 / d), heads, kForwardWaves); }
+
 template <typename T, int D>
 hipError_t forward(const HeadRows &Q, const HeadRows &K, const void *wq, const void *wk, float eps, const RotaryTable &rt, long B,
                    int L, const HeadRows &Qo, const HeadRows &Ko, hipStream_t st) {
     constexpr int TPW = 512 / D;
     const long tokens = B * L, groups = (tokens + TPW - 1) / TPW;
-    const int heads = Q.H + K.H, each = heads_each(groups, heads, kForwardWaves), parts = (heads + each - 1) / each;
+    const int heads = Q.H + K.H, each = forward_each(tokens, heads, D), parts = (heads + each - 1) / each;
     const dim3 grid((unsigned)((groups * parts + 3) / 4));
-    // Results of bfloat16 leave the caches first, up to half of the last-level cache: 84 MB (4 x 1024 tokens of 32 + 8 heads, d = 128)
-    // 18.9 us without and 17.6 with it, 100 MB (16 x 1024, 12 + 12, d = 64) 20.5 and 19.2, and behind it 134 MB 24.1 and 24.3, 268 MB 49.5
-    // and 51.4.  Of float a lane stores two halves of 32 bytes, which then leave apart from each other: 100 MB 18.1 and 20.5.
-    const bool past = sizeof(T) == 2 && 2 * tokens * heads * D * (long)sizeof(T) <= kCacheBytes / 2;
+    const bool past = forward_past(tokens, heads, D, sizeof(T));
 #define DFSS_LAUNCH(U)                                                                                                   \
     if (past) DFSS_PAST(U, sizeof(T) == 2); else DFSS_PAST(U, false)
 #define DFSS_PAST(U, PAST)                                                                                               \
@@ -283,10 +290,7 @@ hipError_t backward(const HeadRows &dQo, const HeadRows &dKo, const HeadRows &Q,
         if (k && qg > kGradGroups - 1) qg = kGradGroups - 1;
         kg = k ? kGradGroups - qg : 0;
     }
-    // A call that leaves little of the last-level cache to others reads x and writes dx past it, so that dy, which was just written, stays:
-    // 202 MB (4 x 2048 tokens of 16 + 16 heads, d = 128) 52.1 us without and 40.6 with it, 403 MB 95.8 and 82.7, float 89.1 and 79.4;
-    // smaller ones find x there, too: 126 MB (4 x 1024, 32 + 8) 31.2 and 34.6, float 151 MB 31.7 and 33.8.
-    const bool past = 3 * tokens * (Q.H + K.H) * D * (long)sizeof(T) > kCacheBytes * 5 / 8;
+    const bool past = backward_past(tokens, Q.H + K.H, D, sizeof(T));
 #define DFSS_LAUNCH(PAST)                                                                                                \
     hipLaunchKernelGGL((k_norm_rotate_grad<T, D, U, PAST>), dim3((unsigned)(qg + kg)), dim3(256), 0, st, dQo, dKo, Q, K, (const T *)wq, \
                        (const T *)wk, eps, rt, tokens, L, dQ, dK, (int)qg, each, part)
@@ -306,6 +310,10 @@ hipError_t launch_norm_rotate(const HeadRows &Q, const HeadRows &K, const void *
     if (f32) return d == 64 ? DFSS_CALL(float, 64) : DFSS_CALL(float, 128);
     return d == 64 ? DFSS_CALL(__bf16, 64) : DFSS_CALL(__bf16, 128);
 #undef DFSS_CALL
+}
+
+NormPlan norm_rotate_plan(long tokens, int heads, int d, int elem) {
+    return NormPlan{forward_each(tokens, heads, d) >= 4 ? 4 : 1, forward_past(tokens, heads, d, elem), backward_past(tokens, heads, d, elem)};
 }
 
 size_t norm_rotate_workspace_bytes(int d) { return (size_t)kGradGroups * d * sizeof(float); }

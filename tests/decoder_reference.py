@@ -110,3 +110,56 @@ def attention(Q, counts, K, V, seen, length, max_len, N, M, scale, causal):
             A[at + i] = (P[:, None] @ torch.where(seen[b][:keys, None], v, 0.0).abs())[:, 0]
         at += n
     return O, A, gap
+
+
+def append_at_once(values, scale, x, table, length, counts, page, max_len, n_pages):
+    """As append, all heads of a page at a time."""
+    exact, at = torch.full_like(values, math.nan), 0
+    limit = min(max_len, table.shape[1] * page)
+    for b, n in enumerate(counts):
+        start = int(length[b]) - n
+        for p in range(max(start, 0) // page, (max(start + n, 0) + page - 1) // page):
+            lo, hi, id = max(start, 0, p * page), min(start + n, limit, (p + 1) * page), int(table[b, p])
+            if lo >= hi or not 0 <= id < n_pages:
+                continue
+            new = x[at + lo - start:at + hi - start].transpose(0, 1)
+            m, e = torch.frexp(new.abs().amax((1, 2)))      # m 2^e with m in [0.5, 1); 448 = 0.875 * 2^9
+            s = torch.where(m > 0, torch.ldexp(torch.ones_like(m), (e - 9 + (m > 0.875).int()).clamp(min=-64)), 2.0 ** -64)
+            if lo > p * page:
+                s = torch.maximum(s, scale[id])
+                values[id, :, :lo - p * page] = nearest(values[id, :, :lo - p * page] * (scale[id] / s)[:, None, None])
+            scale[id] = s
+            exact[id, :, lo - p * page:hi - p * page] = new / s[:, None, None]
+            values[id, :, lo - p * page:hi - p * page] = nearest(new / s[:, None, None])
+        at += n
+    return exact
+
+
+def attention_at_once(Q, counts, K, V, seen, length, max_len, N, M, scale, causal):
+    """As attention, all queries of a sequence at a time."""
+    O, A, gap, at = torch.zeros_like(Q, dtype=torch.float64), torch.zeros_like(Q, dtype=torch.float64), torch.full(Q.shape[:2], math.inf, dtype=torch.float64), 0
+    H = Q.shape[1]
+    for b, n in enumerate(counts):
+        G, keys, rows = H // K[b].shape[0], min(int(length[b]), max_len), slice(at, at + n)
+        at += n
+        if n == 0 or keys <= 0:
+            continue
+        k, v = (x[:, :keys].repeat_interleave(G, 0) for x in (K[b], torch.where(seen[b][:, None], V[b], 0.0)))
+        S = Q[rows].double().transpose(0, 1) @ k.transpose(1, 2)                    # [H, n, keys]
+        hidden = ~seen[b][:keys].expand(n, keys)
+        if causal:
+            hidden = hidden | (torch.arange(keys) > int(length[b]) - n + torch.arange(n)[:, None])
+        S = S.masked_fill(hidden, -math.inf)
+        if N:
+            R = torch.nn.functional.pad(S, (0, -keys % M), value=-math.inf).unflatten(-1, (-1, M))
+            order = torch.sort(R, dim=-1, descending=True, stable=True)
+            if N < M:
+                close = (order.values[..., N - 1] - order.values[..., N]).nan_to_num(nan=math.inf, posinf=math.inf)
+                close[close == 0] = math.inf
+                gap[rows] = close.amin(-1).T
+            S = R.scatter(-1, order.indices[..., N:], -math.inf).flatten(-2)[..., :keys]
+        m = S.amax(-1, keepdim=True)
+        P = torch.where(S == -math.inf, 0.0, torch.exp((S - m.clamp(min=-1e300)) * scale))
+        P = P / P.sum(-1, keepdim=True).clamp(min=1e-300)
+        O[rows], A[rows] = (P @ v).transpose(0, 1), (P @ v.abs()).transpose(0, 1)
+    return O, A, gap

@@ -269,11 +269,13 @@ hipError_t launch_cache_append(const HeadRows &K, const HeadRows &V, int T, cons
     // 27.5; four waves of eight 33.5 (128, 64), of four 28.8.
 #define DFSS_PASSES(D)                                                                                                  \
     if (passes <= 1) DFSS_LAUNCH(D, 1, 1); else if (passes <= 2) DFSS_LAUNCH(D, 1, 2); else if (passes <= 4) DFSS_LAUNCH(D, 1, 4); \
-    else if (passes <= 8) DFSS_LAUNCH(D, 4, 2); else if (passes <= 16) DFSS_LAUNCH(D, 4, 4); else DFSS_LAUNCH(D, 4, 8)
+    else if (passes <= 8) DFSS_LAUNCH(D, 4, 2); else DFSS_LAUNCH(D, 4, 4)
     if (d == 64) {
-        DFSS_PASSES(64);
-    } else {
+        DFSS_PASSES(64);   // (128 rows are 16 passes)
+    } else if (passes <= 16) {
         DFSS_PASSES(128);
+    } else {
+        DFSS_LAUNCH(128, 4, 8);
     }
 #undef DFSS_PASSES
 #undef DFSS_LAUNCH

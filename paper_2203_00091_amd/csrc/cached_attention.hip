@@ -477,11 +477,23 @@ __global__ __launch_bounds__(2 * D) void k_cached_merge(const float *__restrict_
         pack_bf16x2(a0[0], a0[1]), pack_bf16x2(a0[2], a0[3]), pack_bf16x2(a1[0], a1[1]), pack_bf16x2(a1[2], a1[3])};
 }
 
-// 16-row tiles of a workgroup.  32 sequences of up to 4096 keys, us, in tiles of 32 rows and of 128 (cached_wide.hip):
-//   8 key heads, d = 128, pages of 64, 2:4     48 rows 63 and 76, 64 rows 65 and 82, 96 rows 96 and 81, 256 rows 187 and 150
-//   16 key heads, d = 64, pages of 32, full    48 rows 66 and 118, 96 rows 81 and 122, 128 rows 106 and 123, 192 rows 145 and 213
-// and at d = 64 with 2048 rows, 2:4, 2 x 16 heads 150 and 109.
-int row_tiles(long rows, int d) { return rows <= 16 ? 1 : rows <= (d == 64 ? 128 : 64) ? 2 : kWide; }
+// 16-row tiles of a workgroup: 1, 2, or 8 (cached_wide.hip; for its 128 rows a block is converted once, whether they are there or not).
+// Us in tiles of 32 rows and of 128:
+//   d = 128: 64 rows.  32 sequences of up to 4096 keys, 8 key heads, pages of 64
+//     2:4   48 rows 61 and 77, 64 rows 61 and 77, 96 rows 92 and 79, 128 rows 97 and 81
+//     1:2   64 rows 61 and 68, 96 rows 88 and 71;   full  64 rows 59 and 73, 96 rows 84 and 77
+//   d = 64: 192 rows with up to 4096 keys, 128 with more.  16 sequences of up to 4096 keys, 16 key heads, pages of 64, then of 32
+//     2:4   160 rows 82 and 105, 192 rows 90 and 104, 256 rows 117 and 105;   97 and 110, 107 and 110, 140 and 111
+//     1:2   160 rows 73 and 89, 192 rows 77 and 88, 256 rows 102 and 90;   78 and 97, 87 and 98, 114 and 100
+//     full  160 rows 63 and 93, 192 rows 69 and 93, 256 rows 89 and 94;   81 and 97, 90 and 98, 119 and 100
+//     one sequence of 1024, 8 key heads, 192 rows, 2:4: 9.9 and 19.5; in pages of 16 tiles of 32 lose at the end (8 sequences x 12 key heads,
+//     160 rows, 2:4 78 and 64, full 58 and 58)
+//     192 rows of 4 sequences of 6000 x 8 key heads, pages of 64: 2:4 56 and 32, full 49 and 30; of 16 of 8192, 137 and 112, 106 and 102
+//     at 128 rows tiles of 128 win on a full chip (32 x 16 key heads, pages of 32, 2:4 145 and 117) and lose on one in part (one sequence, 9.8 and 19.5)
+int row_tiles(long rows, int max_len, int d) {
+    const long most = d == 128 ? 64 : max_len <= 4096 ? 192 : 128;
+    return rows <= 16 ? 1 : rows <= most ? 2 : kWide;
+}
 
 struct Plan {
     int RT, NW, tiles, target, least, fill;   // fill: `per` is the least possible; NW: waves of a workgroup; target 0: nobody shares
@@ -489,7 +501,7 @@ struct Plan {
 Plan plan(int B, int Hk, int G, int most, int max_len, int d) {
     Plan p;
     const long rows = (long)most * G;
-    p.RT = row_tiles(rows, d);
+    p.RT = row_tiles(rows, max_len, d);
     p.tiles = (int)((rows + 16 * p.RT - 1) / (16 * p.RT));
     const long per_share = (long)Hk * p.tiles, items = B * per_share;   // workgroups of a share, and without shares
     const int blocks = (max_len + KB - 1) / KB;

@@ -24,6 +24,14 @@ def test_attention_over_the_cache():
     assert reached == want | {(64, 1, 16, 0, 0)}
 
 
+@pytest.mark.parametrize("d, keys, most", [(64, 1024, 192), (64, 4096, 192), (64, 4097, 128), (64, 30000, 128), (128, 1024, 64), (128, 9000, 64)])
+def test_rows_of_a_tile(d, keys, most):
+    """The borders where tiles of 128 rows are the faster ones, as measured (128 rows to 192 at d = 64 are not, with few keys)."""
+    for G in (1, 4):
+        tiles = [cases.internal_plan("cached", 8, 12 * G, 12, rows // G, keys, d)[0] for rows in (4, 16, 20, most, most + 4, 2048)]
+        assert tiles == [1, 1, 2, 2, 8, 8]
+
+
 def test_append():
     reached = set()
     for case, want in cases.APPEND:

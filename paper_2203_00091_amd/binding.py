@@ -13,6 +13,7 @@ import os
 import struct
 from dataclasses import dataclass, fields
 from functools import cached_property
+from operator import attrgetter
 
 import torch
 
@@ -807,17 +808,24 @@ def _array(t: torch.Tensor, dtype, shape, device: int | None, what: str) -> int:
     return t.data_ptr()
 
 
+def _kept(slot: str) -> property:
+    """What an object was made of, to be read: the pointers that its calls pass on were taken then."""
+    return property(attrgetter(slot))
+
+
 class Rotary:
     """Rotary positions (``dfss_rotary``): cos, sin float32 [n_pos, rot/2]; pos int32, the position of every token of a
-    call (None: its place in its sequence); pairs (i, i + rot/2), or neighbours if ``interleaved``.  Keeps its tensors."""
-    __slots__ = ("cos", "sin", "pos", "interleaved", "device", "_c")
+    call (None: its place in its sequence); pairs (i, i + rot/2), or neighbours if ``interleaved``.  Keeps its tensors, which
+    cannot be exchanged for others (their contents can): another tensor is another Rotary."""
+    __slots__ = ("_cos", "_sin", "_pos", "_interleaved", "_device", "_c")
+    cos, sin, pos, interleaved, device = map(_kept, __slots__[:5])
 
     def __init__(self, cos, sin, pos=None, interleaved: bool = False):
         shape, f = cos.shape, torch.float32
         if len(shape) != 2:
             raise ValueError(f"cos, sin: expected [n_pos, rot/2], got {list(shape)}")
-        self.cos, self.sin, self.pos, self.interleaved = cos, sin, pos, interleaved
-        self.device = dev = cos.get_device()
+        self._cos, self._sin, self._pos, self._interleaved = cos, sin, pos, interleaved
+        self._device = dev = cos.get_device()
         if not (_current(dev) and cos.dtype is f and sin.dtype is f and sin.shape == shape and sin.get_device() == dev
                 and cos.is_contiguous() and sin.is_contiguous()):
             _array(cos, f, shape, None, "cos"), _array(sin, f, shape, dev, "sin")   # says what is wrong
@@ -828,9 +836,9 @@ class Rotary:
 def _rotary(r: Rotary | None, tokens: int):
     if r is None:
         return None
-    if r.pos is not None and r.pos.numel() != tokens:
-        raise ValueError(f"pos: expected {tokens} positions, got {r.pos.numel()}")
-    if not _current(r.device):
+    if r._pos is not None and r._pos.numel() != tokens:
+        raise ValueError(f"pos: expected {tokens} positions, got {r._pos.numel()}")
+    if not _current(r._device):
         raise ValueError(f"rotary: expected one on the current device, got one on {r.cos.device}")
     return r._c
 
@@ -840,18 +848,21 @@ _CODES = (torch.uint8, torch.float8_e4m3fn)
 
 class Cache:
     """A paged cache of 8 bits (``dfss_cache``): k, v uint8 or float8_e4m3fn [n_pages, Hk, page, d], their scales float32
-    [n_pages, Hk], table int32 [B, width], len int32 [B].  Keeps its tensors."""
-    __slots__ = ("k", "v", "k_scale", "v_scale", "table", "len", "B", "Hk", "d", "device", "_c")
+    [n_pages, Hk], table int32 [B, width], len int32 [B].  Keeps its tensors, which cannot be exchanged for others (their contents
+    can): another table, say, is another Cache."""
+    __slots__ = ("_k", "_v", "_k_scale", "_v_scale", "_table", "_len", "_B", "_Hk", "_d", "_device", "_c")
+    k, v, k_scale, v_scale, table, len, B, Hk, d, device = map(_kept, __slots__[:10])
 
     def __init__(self, k, v, k_scale, v_scale, table, len):
         shape, where, f, i = k.shape, table.shape, torch.float32, torch.int32
         if k.dim() != 4 or table.dim() != 2:
             raise ValueError(f"expected k, v [n_pages, Hk, page, d] and table [B, width], got {list(shape)}, {list(where)}")
-        self.k, self.v, self.k_scale, self.v_scale, self.table, self.len = k, v, k_scale, v_scale, table, len
-        n, self.Hk, page, self.d = shape
-        self.B, width = where
-        scales, codes, lens = (n, self.Hk), k.dtype, (self.B,)
-        self.device = dev = k.get_device()
+        self._k, self._v, self._k_scale, self._v_scale, self._table, self._len = k, v, k_scale, v_scale, table, len
+        n, Hk, page, self._d = shape
+        B, width = where
+        self._Hk, self._B = Hk, B
+        scales, codes, lens = (n, Hk), k.dtype, (B,)
+        self._device = dev = k.get_device()
         if not (codes in _CODES and v.dtype is codes and k_scale.dtype is f and v_scale.dtype is f and table.dtype is i and len.dtype is i
                 and v.shape == shape and k_scale.shape == scales and v_scale.shape == scales and len.shape == lens
                 and _current(dev) and v.get_device() == dev and k_scale.get_device() == dev and v_scale.get_device() == dev
@@ -862,7 +873,7 @@ class Cache:
             _array(k_scale, f, scales, dev, "k_scale"), _array(v_scale, f, scales, dev, "v_scale")
             _array(table, i, where, dev, "table"), _array(len, i, lens, dev, "len")
         self._c = _CACHE.pack(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), table.data_ptr(), len.data_ptr(),
-                              n, self.Hk, page, width)
+                              n, Hk, page, width)
 
 
 def _scratch(ws: torch.Tensor | None) -> int | None:
@@ -966,10 +977,10 @@ def _offsets(cu: torch.Tensor | None, s: Shape):
 
 
 def _cache(c: Cache, s: Shape):
-    if c.B != s.B or c.d != s.d:
-        raise ValueError(f"cache: expected {s.B} sequences and head size {s.d}, got {c.B} and {c.d}")
-    if not _current(c.device):
-        raise ValueError(f"cache: expected one on the current device, got one on {c.k.device}")
+    if c._B != s.B or c._d != s.d:
+        raise ValueError(f"cache: expected {s.B} sequences and head size {s.d}, got {c._B} and {c._d}")
+    if not _current(c._device):
+        raise ValueError(f"cache: expected one on the current device, got one on {c._k.device}")
     return c._c
 
 
@@ -1001,9 +1012,9 @@ def _attention_cached(name: str, Q, cu, cache: Cache, s: Shape, scale: float, ca
     if ws is not None:
         need, w = ws.numel() * ws.element_size(), _scratch(ws)
     else:
-        need = s._call.cached_ws.get(cache.Hk)      # (of a valid shape it depends on nothing else of the cache)
+        need = s._call.cached_ws.get(cache._Hk)      # (of a valid shape it depends on nothing else of the cache)
         if not need:
-            need = s._call.cached_ws[cache.Hk] = L.dfss_cached_workspace_bytes(s._call.ref, c)
+            need = s._call.cached_ws[cache._Hk] = L.dfss_cached_workspace_bytes(s._call.ref, c)
         if need:
             ws = _alloc_bytes(need, Q.device)
             w = ws.data_ptr()

@@ -508,6 +508,8 @@ Plan plan(int B, int Hk, int G, int most, int max_len, int d) {
     // Eight waves where that is still one workgroup for each compute unit at most: the wave's own chain of blocks sets the time there
     // (4 sequences of 32768 keys, 8 key heads, d = 128, shared: 42 + 5 us, with four waves 48 + 8).  Four where workgroups follow each
     // other, since a new one then starts sooner (128 sequences of 2048 keys, 16 heads, d = 64: 77, with eight 87, both with all codes through the caches).
+    // (Also of shares of few blocks: eight waves and four, us, 1 sequence of 6000 keys, 8 key heads, d = 64 10.9 and 11.6, of 16384 15.6 and 18.9,
+    // d = 128 13.7 and 13.6, 18.8 and 21.8; 4 of 8192 14.8 and 15.4, 19.4 and 19.9; 1 of 32768, 2 heads 18.1 and 26.4, 20.3 and 28.1.)
     p.NW = items <= 256 || p.RT == kWide ? 8 : 4;
     p.target = 0;
     p.least = p.NW;
@@ -519,8 +521,6 @@ Plan plan(int B, int Hk, int G, int most, int max_len, int d) {
     // Five blocks a wave cost less than a second kernel, 5 us (24 sequences of 2500 keys, 4 key heads, d = 64: 12.4 alone, 11.9 + 4.6
     // shared).  (Behind 2^30 the sum of blocks that the shares are counted in would pass 32 bits.)
     if (blocks <= 5 * p.NW || (long)B * blocks > 1 << 30) return p;
-    // Few blocks in all: shares of four blocks, so that there are twice as many of them.
-    if (items * blocks <= 4096 && p.RT != kWide) p.NW = 4;
     // Workgroups that the chip holds at a time, by their registers and LDS.  Where the sequences alone are that many, sharing only
     // evens their lengths out, which is worth the merge for long ones alone (64 sequences of up to 4096 keys, 8 key heads, d = 128:
     // 81 us alone, 96 + 6 shared, likewise), and with four rounds of them lengths even out by themselves.

@@ -17,7 +17,7 @@ def attend_counts(B, queries):
 ATTEND = [
     ((0, 8, 1, 40, 1, 1200), (1, 4, 0, 0)),
     ((0, 2, 3, 5, 1, 2500), (1, 8, 0, 0)),
-    ((0, 2, 2, 3, 3, 6000), (1, 4, 1, 0)),
+    ((0, 4, 2, 70, 1, 1400), (1, 4, 1, 0)),
     ((0, 8, 2, 40, 2, 1400), (1, 4, 1, 1)),
     ((0, 4, 1, 8, 1, 8300), (1, 8, 1, 0)),
     ((128, 8, 1, 8, 1, 4200), (1, 8, 1, 1)),
@@ -26,7 +26,7 @@ ATTEND = [
     ((64, 12, 1, 6, 3, 5120), (1, 16, 0, 0)),
     ((0, 8, 2, 40, 11, 600), (2, 4, 0, 0)),
     ((0, 2, 4, 5, 9, 2500), (2, 8, 0, 0)),
-    ((0, 2, 2, 3, 20, 2600), (2, 4, 1, 0)),
+    ((0, 4, 2, 70, 11, 1400), (2, 4, 1, 0)),
     ((0, 8, 2, 40, 12, 1400), (2, 4, 1, 1)),
     ((0, 4, 2, 8, 13, 8300), (2, 8, 1, 0)),
     ((0, 8, 2, 8, 9, 5200), (2, 8, 1, 1)),

@@ -32,6 +32,13 @@ def test_rows_of_a_tile(d, keys, most):
         assert tiles == [1, 1, 2, 2, 8, 8]
 
 
+@pytest.mark.parametrize("d", BOTH)
+def test_shares_of_few_blocks_have_eight_waves(d):
+    """As measured: sequences that are few for the chip are walked by eight waves to a workgroup, however few blocks they have in all."""
+    for B, Hk, queries, keys in ((1, 8, 1, 6000), (1, 2, 1, 32768), (4, 8, 1, 8192), (2, 8, 8, 8192)):
+        assert cases.internal_plan("cached", B, 4 * Hk, Hk, queries, keys, d)[1:3] == (8, 1)
+
+
 def test_append():
     reached = set()
     for case, want in cases.APPEND:

@@ -514,10 +514,12 @@ Plan plan(int B, int Hk, int G, int most, int max_len, int d) {
     p.target = 0;
     p.least = p.NW;
     p.fill = 0;
-    // d = 64: sixteen waves walk 80 blocks before a second kernel pays.  12 heads a sequence, 4096 keys, us, sixteen waves, and eight
-    // that share the keys with others: 1 sequence 12.7 and 6.1 + 5, 8 of them 14.3 and 13.3 + 5, 20 21.0 and 29.7 + 5; eight waves are
-    // enough up to 40 blocks (2000 keys: 9.5 and 9.2).
-    if (d == 64 && p.RT == 1 && items <= 256 && blocks > 40 && blocks <= 80) p.NW = 16;
+    // d = 64: sixteen waves walk 80 blocks before a second kernel pays, but for few workgroups, whose sharing is all the rest of the chip's.
+    // Us of sixteen waves and of eight that share, merge included, 2600 and 4096 keys: 12 workgroups 9.8 and 9.8, 12.5 and 9.9; 48 10.8 and
+    // 11.6, 13.9 and 13.2; 64 10.8 and 13.0, 13.6 and 14.6; 96 11.0 and 14.9, 13.8 and 16.8; 240 (4096) 21.2 and 30.8.  Eight waves are enough
+    // up to 40 blocks (2000 keys, 12 workgroups 8.9 and 8.9, 96 10.1 and 10.3).  (At d = 128 they would have to spill 142 to 174
+    // registers.)
+    if (d == 64 && p.RT == 1 && items > 48 && items <= 256 && blocks > 40 && blocks <= 80) p.NW = 16;
     // Five blocks a wave cost less than a second kernel, 5 us (24 sequences of 2500 keys, 4 key heads, d = 64: 12.4 alone, 11.9 + 4.6
     // shared).  (Behind 2^30 the sum of blocks that the shares are counted in would pass 32 bits.)
     if (blocks <= 5 * p.NW || (long)B * blocks > 1 << 30) return p;

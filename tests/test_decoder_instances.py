@@ -39,6 +39,13 @@ def test_shares_of_few_blocks_have_eight_waves(d):
         assert cases.internal_plan("cached", B, 4 * Hk, Hk, queries, keys, d)[1:3] == (8, 1)
 
 
+def test_sixteen_waves_are_for_more_than_a_few_workgroups():
+    """As measured: up to 48 workgroups of 41 to 80 blocks leave so much of the chip idle that others share their keys."""
+    for B, Hk, want in ((1, 12, (8, 1)), (4, 12, (8, 1)), (7, 7, (16, 0)), (8, 12, (16, 0)), (20, 12, (16, 0))):
+        for keys in (2600, 5120):
+            assert cases.internal_plan("cached", B, Hk, Hk, 1, keys, 64)[1:3] == want
+
+
 def test_append():
     reached = set()
     for case, want in cases.APPEND:

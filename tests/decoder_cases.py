@@ -16,7 +16,10 @@ def attend_counts(B, queries):
 #   -> 16-row tiles and waves of a workgroup, whether keys are shared, whether with the least shares
 ATTEND = [
     ((0, 8, 1, 40, 1, 1200), (1, 4, 0, 0)),
-    ((0, 2, 3, 5, 1, 2500), (1, 8, 0, 0)),
+    ((0, 2, 3, 5, 1, 1500), (1, 8, 0, 0)),
+    ((64, 2, 3, 5, 1, 2500), (1, 8, 0, 0)),
+    ((128, 2, 3, 5, 1, 1600), (1, 8, 1, 0)),
+    ((128, 14, 1, 7, 2, 2500), (1, 8, 0, 0)),
     ((0, 4, 2, 70, 1, 1400), (1, 4, 1, 0)),
     ((0, 8, 2, 40, 2, 1400), (1, 4, 1, 1)),
     ((0, 4, 1, 8, 1, 8300), (1, 8, 1, 0)),
@@ -26,12 +29,13 @@ ATTEND = [
     ((64, 3, 4, 4, 1, 2600), (1, 8, 1, 0)),
     ((64, 12, 1, 6, 3, 5120), (1, 16, 0, 0)),
     ((0, 8, 2, 40, 11, 600), (2, 4, 0, 0)),
-    ((0, 2, 4, 5, 9, 2500), (2, 8, 0, 0)),
+    ((0, 2, 4, 5, 9, 1500), (2, 8, 0, 0)),
     ((0, 4, 2, 70, 11, 1400), (2, 4, 1, 0)),
     ((0, 8, 2, 40, 12, 1400), (2, 4, 1, 1)),
     ((0, 4, 2, 8, 13, 8300), (2, 8, 1, 0)),
     ((0, 8, 2, 8, 9, 5200), (2, 8, 1, 1)),
     ((0, 2, 2, 5, 150, 700), (8, 8, 0, 0)),
+    ((0, 2, 2, 5, 150, 1600), (8, 8, 1, 0)),
     ((0, 2, 2, 3, 150, 2700), (8, 8, 1, 0)),
     ((0, 8, 2, 4, 150, 2700), (8, 8, 1, 1)),
 ]

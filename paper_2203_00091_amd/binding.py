@@ -808,7 +808,7 @@ def _array(t: torch.Tensor, dtype, shape, device: int | None, what: str) -> int:
     return t.data_ptr()
 
 
-def _kept(slot: str) -> property:
+def _read_only(slot: str) -> property:
     """What an object was made of, to be read: the pointers that its calls pass on were taken then."""
     return property(attrgetter(slot))
 
@@ -818,7 +818,7 @@ class Rotary:
     call (None: its place in its sequence); pairs (i, i + rot/2), or neighbours if ``interleaved``.  Keeps its tensors, which
     cannot be exchanged for others (their contents can): another tensor is another Rotary."""
     __slots__ = ("_cos", "_sin", "_pos", "_interleaved", "_device", "_c")
-    cos, sin, pos, interleaved, device = map(_kept, __slots__[:5])
+    cos, sin, pos, interleaved, device = map(_read_only, __slots__[:5])
 
     def __init__(self, cos, sin, pos=None, interleaved: bool = False):
         shape, f = cos.shape, torch.float32
@@ -851,7 +851,7 @@ class Cache:
     [n_pages, Hk], table int32 [B, width], len int32 [B].  Keeps its tensors, which cannot be exchanged for others (their contents
     can): another table, say, is another Cache."""
     __slots__ = ("_k", "_v", "_k_scale", "_v_scale", "_table", "_len", "_B", "_Hk", "_d", "_device", "_c")
-    k, v, k_scale, v_scale, table, len, B, Hk, d, device = map(_kept, __slots__[:10])
+    k, v, k_scale, v_scale, table, len, B, Hk, d, device = map(_read_only, __slots__[:10])
 
     def __init__(self, k, v, k_scale, v_scale, table, len):
         shape, where, f, i = k.shape, table.shape, torch.float32, torch.int32

@@ -514,12 +514,12 @@ Plan plan(int B, int Hk, int G, int most, int max_len, int d) {
     p.target = 0;
     p.least = p.NW;
     p.fill = 0;
-    // d = 64: sixteen waves walk 80 blocks before a second kernel pays, but for few workgroups, whose sharing is all the rest of the chip's.
-    // Us of sixteen waves and of eight that share, merge included, 2600 and 4096 keys: 12 workgroups 9.8 and 9.8, 12.5 and 9.9; 48 10.8 and
-    // 11.6, 13.9 and 13.2; 64 10.8 and 13.0, 13.6 and 14.6; 96 11.0 and 14.9, 13.8 and 16.8; 240 (4096) 21.2 and 30.8.  Eight waves are enough
-    // up to 40 blocks (2000 keys, 12 workgroups 8.9 and 8.9, 96 10.1 and 10.3).  (At d = 128 they would have to spill 142 to 174
-    // registers.)
-    if (d == 64 && p.RT == 1 && items > 48 && items <= 256 && blocks > 40 && blocks <= 80) p.NW = 16;
+    // d = 64: sixteen waves walk 80 blocks before a second kernel pays.  Us of sixteen waves and of eight that share, merge included, 2600 and
+    // 4096 keys, in a graph: 12 workgroups 9.8 and 9.8, 12.5 and 9.9; 48 10.8 and 11.6, 13.9 and 13.2; 64 10.8 and 13.0, 13.6 and 14.6; 96 11.0 and
+    // 14.9, 13.8 and 16.8; 240 (4096) 21.2 and 30.8.  Called one by one, two kernels and their workspace are 4 us more of the host's time
+    // (12 workgroups, 4096 keys: 12.3 and 15.7 a call), which few workgroups would gain back in graphs alone.  Eight waves are enough up to 40
+    // blocks (2000 keys, 12 workgroups 8.9 and 8.9, 96 10.1 and 10.3).  (At d = 128 they would have to spill 142 to 174 registers.)
+    if (d == 64 && p.RT == 1 && items <= 256 && blocks > 40 && blocks <= 80) p.NW = 16;
     // Five blocks a wave cost less than a second kernel, 5 us, unless a block is long (d = 128, tiles of 128 rows) and so much of the chip
     // idle that sharing makes one of them of the five.  Us alone and shared, merge included:
     //   d = 64, one query                  2500 keys, 8 workgroups 10.1 and 10.3, 96 11.5 and 13.9, 128 11.9 and 15.5

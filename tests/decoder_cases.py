@@ -25,8 +25,7 @@ ATTEND = [
     ((0, 4, 1, 8, 1, 8300), (1, 8, 1, 0)),
     ((128, 8, 1, 8, 1, 4200), (1, 8, 1, 1)),
     ((64, 16, 1, 8, 1, 5200), (1, 8, 1, 1)),
-    ((64, 7, 4, 7, 1, 2600), (1, 16, 0, 0)),
-    ((64, 3, 4, 4, 1, 2600), (1, 8, 1, 0)),
+    ((64, 3, 4, 4, 1, 2600), (1, 16, 0, 0)),
     ((64, 12, 1, 6, 3, 5120), (1, 16, 0, 0)),
     ((0, 8, 2, 40, 11, 600), (2, 4, 0, 0)),
     ((0, 2, 4, 5, 9, 1500), (2, 8, 0, 0)),

@@ -39,16 +39,9 @@ def test_shares_of_few_blocks_have_eight_waves(d):
         assert cases.internal_plan("cached", B, 4 * Hk, Hk, queries, keys, d)[1:3] == (8, 1)
 
 
-def test_sixteen_waves_are_for_more_than_a_few_workgroups():
-    """As measured: up to 48 workgroups of 41 to 80 blocks leave so much of the chip idle that others share their keys."""
-    for B, Hk, want in ((1, 12, (8, 1)), (4, 12, (8, 1)), (7, 7, (16, 0)), (8, 12, (16, 0)), (20, 12, (16, 0))):
-        for keys in (2600, 5120):
-            assert cases.internal_plan("cached", B, Hk, Hk, 1, keys, 64)[1:3] == want
-
-
 def test_who_walks_five_blocks_and_who_three():
     """As measured: few workgroups of long blocks share their keys from 25 blocks on, others from 41."""
-    for d, B, Hk, queries, most in ((64, 1, 8, 1, 40), (128, 1, 8, 1, 24), (128, 8, 8, 1, 24), (128, 12, 8, 1, 40), (128, 8, 8, 8, 24), (64, 1, 8, 256, 24), (64, 2, 8, 256, 40),
+    for d, B, Hk, queries, most in ((64, 1, 8, 1, 80), (64, 1, 8, 8, 40), (128, 1, 8, 1, 24), (128, 8, 8, 1, 24), (128, 12, 8, 1, 40), (128, 8, 8, 8, 24), (64, 1, 8, 256, 24), (64, 2, 8, 256, 40),
                                     (128, 1, 8, 256, 24), (128, 2, 8, 256, 40)):
         shared = [cases.internal_plan("cached", B, 4 * Hk, Hk, queries, keys, d)[2] for keys in (64 * most, 64 * most + 1)]
         assert shared == [0, 1], (d, B, Hk, queries)

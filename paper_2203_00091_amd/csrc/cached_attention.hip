@@ -521,15 +521,16 @@ Plan plan(int B, int Hk, int G, int most, int max_len, int d) {
     // blocks (2000 keys, 12 workgroups 8.9 and 8.9, 96 10.1 and 10.3).  (At d = 128 they would have to spill 142 to 174 registers.)
     if (d == 64 && p.RT == 1 && items <= 256 && blocks > 40 && blocks <= 80) p.NW = 16;
     // Five blocks a wave cost less than a second kernel, 5 us, unless a block is long (d = 128, tiles of 128 rows) and so much of the chip
-    // idle that sharing makes one of them of the five.  Us alone and shared, merge included:
+    // idle that sharing makes one of them of the five.  Us alone and shared, merge included, in a graph; shared calls one by one are 16 us
+    // of the host's time, so that no border stands where alone is less:
     //   d = 64, one query                  2500 keys, 8 workgroups 10.1 and 10.3, 96 11.5 and 13.9, 128 11.9 and 15.5
-    //   d = 128, one query                 1600 and 2500 keys, 8 workgroups 13.0 and 12.1, 18.4 and 12.3; 64 14.4 and 13.9, 19.1 and 15.9; 96 14.6
-    //                                      and 16.3, 19.3 and 19.2; 128 14.8 and 18.3, 19.5 and 20.9; 1100 keys, 8 workgroups 10.9 and 12.4
+    //   d = 128, one query                 2100 and 2500 keys, 8 workgroups 15.7 and 12.1, 18.4 and 12.3; 64 16.6 and 14.8, 19.1 and 15.9; 96 16.8
+    //                                      and 17.3, 19.3 and 19.2; 128 17.0 and 19.3, 19.5 and 20.9
     //   d = 128, 8 queries x 4 heads       1600 and 2500 keys, 8 workgroups 17.3 and 16.2, 22.2 and 16.8; 64 18.1 and 18.5, 23.2 and 20.6
     //   tiles of 128 rows, d = 64, 128     1600 keys, 16 workgroups 25.9 and 17.5, 32.8 and 22.3; 64 25.9 and 21.4, 32.8 and 29.5; 128 26.0
     //                                      and 26.9, 34.1 and 36.7
     // (Behind 2^30 the sum of blocks that the shares are counted in would pass 32 bits.)
-    const int walk = items <= 64 && (d == 128 || p.RT == kWide) ? 3 : 5;
+    const int walk = items > 64 ? 5 : p.RT == kWide ? 3 : d == 128 ? 4 : 5;
     if (blocks <= walk * p.NW || (long)B * blocks > 1 << 30) return p;
     // Workgroups that the chip holds at a time, by their registers and LDS.  Where the sequences alone are that many, sharing only
     // evens their lengths out, which is worth the merge for long ones alone (64 sequences of up to 4096 keys, 8 key heads, d = 128:

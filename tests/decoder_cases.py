@@ -18,7 +18,7 @@ ATTEND = [
     ((0, 8, 1, 40, 1, 1200), (1, 4, 0, 0)),
     ((0, 2, 3, 5, 1, 1500), (1, 8, 0, 0)),
     ((64, 2, 3, 5, 1, 2500), (1, 8, 0, 0)),
-    ((128, 2, 3, 5, 1, 1600), (1, 8, 1, 0)),
+    ((128, 2, 3, 5, 1, 2100), (1, 8, 1, 0)),
     ((128, 14, 1, 7, 2, 2500), (1, 8, 0, 0)),
     ((0, 4, 2, 70, 1, 1400), (1, 4, 1, 0)),
     ((0, 8, 2, 40, 2, 1400), (1, 4, 1, 1)),

@@ -130,3 +130,15 @@ def test_generation_is_what_a_prompt_at_once_is(d, page, mode):
     tol = half * want.abs() + (half + 1e-5) * (amount + want.abs()) * 1.01
     for got in (O, torch.cat([o for _, o in steps]), torch.cat([o for _, o in chunks])):
         assert float(((got.cpu().double() - want).abs() - tol)[clear].max()) <= 0
+
+
+@pytest.mark.parametrize("B", [64, 65, 4096, 4097, 5000])
+def test_append_finds_its_sequence_among_many(B):
+    """One token to most sequences, none to some, and a prompt here and there."""
+    a = Append((16, 64, 1, [((5 * i) % 33, 0 if i % 5 == 2 else 40 if i % 701 == 63 else 1) for i in range(B)], False, 0, False), 93)
+    cache = a.call()
+    for x, codes, scale, got, got_scale in ((a.rows[:, 1:2], a.k, a.k_scale, cache.k, cache.k_scale), (a.rows[:, 2:], a.v, a.v_scale, cache.v, cache.v_scale)):
+        values, want = ref.codes_to_values(codes), scale.double().clone()
+        ref.append_at_once(values, want, x.cpu().double(), a.table, a.lengths, a.counts, 16, a.max_len, a.n_pages)
+        assert torch.equal(got_scale.cpu().double(), want)
+        assert torch.equal(ref.codes_to_values(got.cpu()).nan_to_num(nan=999.0), values.nan_to_num(nan=999.0))
